@@ -227,6 +227,113 @@ mca_status mca_attention_forward_noalloc(const mca_forward_desc* desc, const voi
                                          const void* X, const void* W_v, const void* prepared,
                                          float* Y, int32_t* r, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Exact attention with its gradient: the layer that MCA approximates, as it is trained, and
+ * as single tokens are served.
+ *
+ * Shapes: B = batch, n_q = q_len, n_k = kv_len (padded lengths), H = heads, H_k = kv_heads
+ * (divides H; query head h reads key head h / (H / H_k)), 64 columns per head.
+ *   Q, Y, dY, dQ : [B, n_q, H * 64]      K, V, dK, dV : [B, n_k, H_k * 64]      of `dtype`
+ *   lse          : [B, H, n_q] float32
+ *   bias table   : [bias_buckets, H] of `dtype`, row-major
+ * Query row i of batch row b is at position p = q_pos[b] + i, key row j at position j. With
+ * the batch row's lengths, query i < q_lens[b] attends key j < kv_lens[b] when
+ *   causal = 0 or j <= p, and
+ *   window = 0 or |p - j| <= window / 2 or p = 0 or j = 0 (the local window with a global
+ *   first token of mca_forward_desc), and
+ *   its bias is above -1e30 (a bias table value of -1e30 or less masks its pairs).
+ *   S_ij = scale q_i . k_j + bias_table[bucket(j - p), h]
+ *   lse_i = log sum_j exp S_ij,  P_ij = exp(S_ij - lse_i),  y_i = sum_j P_ij v_j
+ * over the attended keys. A query that attends none, and every row i >= q_lens[b], has
+ * y_i = 0, lse_i = -infinity and no part in any gradient. Key rows at or past kv_lens[b], and
+ * rows of Q, Y and dY at or past q_lens[b], are not read; their rows of dK, dV and dQ are 0.
+ * Backward, from dY, Y and lse of the forward call with the same desc:
+ *   dP_ij = dy_i . v_j,  D_i = dy_i . y_i,  dS_ij = P_ij (dP_ij - D_i)
+ *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dy_i
+ *   (the sums of dk and dv run over the H / H_k query heads of the key head too)
+ *   dbias_table[c, h] = sum of dS_ij over the pairs of head h in bucket c, all batch rows
+ * Logits, softmax statistics and all sums are float32; with bfloat16 inputs P and dS enter
+ * their matrix products rounded to bfloat16, and results are rounded once.
+ * Q, K, V, dY and the bias are expected to be finite (the bias: or masking); a non-finite
+ * value in an attended row makes results that depend on it unspecified.
+ *
+ * Buckets of a relative position r = j - p (a learned bias that distinguishes near distances
+ * one by one and far ones in ranges that grow): n = bias_buckets, d = max(-r, 0); or, when
+ * bias_bidirectional, n = bias_buckets / 2, d = |r|, and n is added to the bucket when r > 0.
+ * With E = n / 2, m = n - E and Dm = bias_max_distance: d < E is in bucket d, any other d in
+ * bucket E + k for the largest k < m with d >= E (Dm / E)^(k / m), decided exactly.
+ */
+typedef struct mca_exact_desc {
+  int64_t batch;     /* B >= 1 */
+  int64_t q_len;     /* n_q >= 1 */
+  int64_t kv_len;    /* n_k >= 1 */
+  int64_t heads;     /* H, 1 .. 1024 */
+  int64_t kv_heads;  /* H_k, divides H */
+  int64_t d_head;    /* must be 64 (MCA_ERR_UNSUPPORTED otherwise) */
+  int32_t dtype;     /* mca_dtype of every matrix and of the bias table */
+  int32_t causal;    /* 0 or 1 */
+  int64_t window;    /* 0, or an even number of keys */
+  double scale;      /* of the logits; finite and > 0 */
+  /* device [B] int32 or NULL: valid rows (clamped to 0 .. n_q and 0 .. n_k; NULL = all) and the
+     position of each batch row's first query (clamped to +-2^26; NULL = 0). Need 4-byte
+     alignment only. */
+  const int32_t* q_lens;
+  const int32_t* kv_lens;
+  const int32_t* q_pos;
+  const void* bias_table;     /* device [bias_buckets, H], or NULL for no bias */
+  int32_t bias_buckets;       /* 2 .. 128; even and >= 4 when bidirectional */
+  int32_t bias_max_distance;  /* Dm, E < Dm <= 256 */
+  int32_t bias_bidirectional; /* 0 or 1 */
+  int32_t reserved;           /* 0 */
+} mca_exact_desc;
+
+/* A [batch, rows, heads * 64] tensor: columns contiguous, strides in elements. `data` is
+   16-byte aligned and the strides are multiples of 16 bytes; row_stride is at least the row's
+   width and below 2^25 bytes. Inputs may repeat rows over the batch (batch_stride 0); the
+   rows of outputs must not overlap one another, an input or another output. */
+typedef struct mca_rows {
+  void* data;
+  int64_t batch_stride;
+  int64_t row_stride;
+} mca_rows;
+
+/*
+ * Bytes of device workspace of mca_exact_attention_forward (backward = 0; may be 0) or
+ * mca_exact_attention_backward (backward = 1) for `desc` (host only). Errors: as their
+ * checks of desc.
+ */
+mca_status mca_exact_workspace_size(const mca_exact_desc* desc, int backward, size_t* bytes);
+
+/*
+ * Y and lse of exact attention. `workspace` may be NULL when its size is 0; its contents on
+ * entry do not matter. Errors: MCA_ERR_INVALID_ARGUMENT (null pointer, size < 1, kv_heads
+ * that does not divide heads, bad scale, window, bias sizes, strides or alignment, reserved
+ * not 0, a problem too large for one launch), MCA_ERR_UNSUPPORTED (d_head != 64),
+ * MCA_ERR_WORKSPACE_TOO_SMALL, MCA_ERR_HIP.
+ */
+mca_status mca_exact_attention_forward(const mca_exact_desc* desc, const mca_rows* Q, const mca_rows* K,
+                                       const mca_rows* V, const mca_rows* Y, float* lse, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of exact attention: dQ, dK, dV and, when desc has a bias table, dbias_table
+ * [bias_buckets, H] (`dtype`; NULL otherwise). The values are written, not added to. Q, K, V,
+ * the lengths and the bias as in the forward call that gave Y and lse. Errors: as
+ * mca_exact_attention_forward.
+ */
+mca_status mca_exact_attention_backward(const mca_exact_desc* desc, const mca_rows* dY, const mca_rows* Q,
+                                        const mca_rows* K, const mca_rows* V, const mca_rows* Y, const float* lse,
+                                        const mca_rows* dQ, const mca_rows* dK, const mca_rows* dV, void* dbias_table,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The bucket of every relative position r = -max_distance .. max_distance, at out[r +
+ * max_distance] (host array of 2 max_distance + 1; positions further away share the bucket of
+ * the end). Host only. Errors: MCA_ERR_INVALID_ARGUMENT for sizes that mca_exact_desc refuses
+ * or a null pointer.
+ */
+mca_status mca_relative_buckets(int32_t buckets, int32_t max_distance, int32_t bidirectional, int32_t* out);
+
 /* Static description of a status code (an mca_status value; any other value gives
    "MCA_ERR_UNKNOWN"). */
 const char* mca_status_string(int status);

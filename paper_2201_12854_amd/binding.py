@@ -67,6 +67,33 @@ class ForwardDesc(ctypes.Structure):
     ]
 
 
+class ExactDesc(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int64),
+        ("q_len", ctypes.c_int64),
+        ("kv_len", ctypes.c_int64),
+        ("heads", ctypes.c_int64),
+        ("kv_heads", ctypes.c_int64),
+        ("d_head", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("causal", ctypes.c_int32),
+        ("window", ctypes.c_int64),
+        ("scale", ctypes.c_double),
+        ("q_lens", ctypes.c_void_p),
+        ("kv_lens", ctypes.c_void_p),
+        ("q_pos", ctypes.c_void_p),
+        ("bias_table", ctypes.c_void_p),
+        ("bias_buckets", ctypes.c_int32),
+        ("bias_max_distance", ctypes.c_int32),
+        ("bias_bidirectional", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
 class MCAError(RuntimeError):
     def __init__(self, status: int, where: str, detail: str):
         self.status = status
@@ -114,6 +141,15 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.mca_profiler_collect.restype = ctypes.c_int
     lib.mca_profiler_destroy.argtypes = [vp]
     lib.mca_profiler_destroy.restype = ctypes.c_int
+    desc, rows = ctypes.POINTER(ExactDesc), ctypes.POINTER(Rows)
+    lib.mca_exact_workspace_size.argtypes = [desc, ctypes.c_int, ctypes.POINTER(sz)]
+    lib.mca_exact_workspace_size.restype = ctypes.c_int
+    lib.mca_exact_attention_forward.argtypes = [desc, rows, rows, rows, rows, vp, vp, sz, vp]
+    lib.mca_exact_attention_forward.restype = ctypes.c_int
+    lib.mca_exact_attention_backward.argtypes = [desc, rows, rows, rows, rows, rows, vp, rows, rows, rows, vp, vp, sz, vp]
+    lib.mca_exact_attention_backward.restype = ctypes.c_int
+    lib.mca_relative_buckets.argtypes = [i32, i32, i32, ctypes.POINTER(i32)]
+    lib.mca_relative_buckets.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -341,3 +377,228 @@ class ForwardPlan:
         st = self._fn(*self._args, self._stream)
         if st != MCA_OK:
             _check(st, "mca_attention_forward")
+
+
+# ---------------------------------------------------------------------------- exact attention
+@dataclass
+class RelativeBias:
+    """A learned relative position bias: ``table`` [buckets, heads] (the layer's dtype, on its
+    device, contiguous). The logit of a query at position p and a key at j gets
+    ``table[bucket(j - p), head]``; ``relative_buckets`` gives the buckets."""
+
+    table: object
+    max_distance: int = 128
+    bidirectional: bool = True
+
+
+def relative_buckets(buckets: int, max_distance: int = 128, bidirectional: bool = True) -> list:
+    """The bucket of every relative position -max_distance .. max_distance (further ones share the
+    end's), as a list of 2 max_distance + 1 integers."""
+    n = 2 * int(max_distance) + 1
+    out = (ctypes.c_int32 * max(n, 1))()
+    _check(load_library().mca_relative_buckets(int(buckets), int(max_distance), int(bool(bidirectional)), out),
+           "mca_relative_buckets")
+    return list(out)
+
+
+@dataclass
+class ExactResult:
+    Y: object
+    lse: object
+
+
+@dataclass
+class ExactGradients:
+    dQ: object
+    dK: object
+    dV: object
+    dbias: object = None
+
+
+def _exact_rows(name, t, shape, like) -> Rows:
+    if not t.is_cuda or t.device != like.device or t.dtype != like.dtype:
+        raise ValueError(f"{name} must be a {like.dtype} tensor on {like.device}")
+    if tuple(t.shape) != tuple(shape) or t.stride(2) != 1:
+        raise ValueError(f"{name} must be {list(shape)} with contiguous columns (got {list(t.shape)}, strides {t.stride()})")
+    # a row or batch stride that nothing steps over may be anything
+    row = t.stride(1) if shape[1] > 1 else shape[2]
+    return Rows(t.data_ptr(), t.stride(0) if shape[0] > 1 else 0, row)
+
+
+class _ExactCall:
+    """The checked arguments of a forward or backward call. Keeps every tensor it points to."""
+
+    def __init__(self, Q, K, V, heads, kv_heads, scale, q_lens, kv_lens, q_pos, causal, window, bias):
+        import torch
+
+        if not Q.is_cuda or Q.dim() != 3 or K.dim() != 3 or V.dim() != 3:
+            raise ValueError("Q, K and V must be 3-D device tensors")
+        kv_heads = heads if kv_heads is None else kv_heads
+        (B, nq, _), nk = Q.shape, K.shape[1]
+        self.q_shape, self.k_shape, self.device = (B, nq, heads * 64), (B, nk, kv_heads * 64), Q.device
+        self.dtype, self.lse_shape = Q.dtype, (B, heads, nq)
+        self.q, self.k, self.v = (_exact_rows(n, t, s, Q) for n, t, s in
+                                  (("Q", Q, self.q_shape), ("K", K, self.k_shape), ("V", V, self.k_shape)))
+        for name, t in (("q_lens", q_lens), ("kv_lens", kv_lens), ("q_pos", q_pos)):
+            if t is not None and (t.dtype != torch.int32 or t.shape != (B,) or t.device != Q.device or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous int32 [{B}] on {Q.device}")
+        d = self.desc = ExactDesc()
+        d.batch, d.q_len, d.kv_len, d.heads, d.kv_heads, d.d_head = B, nq, nk, heads, kv_heads, 64
+        d.dtype, d.causal, d.window = _dtype_code(Q), int(bool(causal)), int(window)
+        d.scale = 0.125 if scale is None else float(scale)
+        d.q_lens, d.kv_lens, d.q_pos = _ptr(q_lens), _ptr(kv_lens), _ptr(q_pos)
+        self.table = None
+        if bias is not None:
+            t = self.table = bias.table
+            if t.dim() != 2 or t.shape[1] != heads or t.dtype != Q.dtype or t.device != Q.device or not t.is_contiguous():
+                raise ValueError(f"bias.table must be a contiguous {Q.dtype} [buckets, {heads}] on {Q.device}")
+            d.bias_table, d.bias_buckets = t.data_ptr(), t.shape[0]
+            d.bias_max_distance, d.bias_bidirectional = int(bias.max_distance), int(bool(bias.bidirectional))
+        self.like = Q
+        self._keep = (Q, K, V, q_lens, kv_lens, q_pos, bias)
+
+    def rows(self, name, t, shape) -> Rows:
+        return _exact_rows(name, t, shape, self.like)
+
+    def check_lse(self, lse):
+        import torch
+
+        if lse.dtype != torch.float32 or tuple(lse.shape) != self.lse_shape or lse.device != self.device or not lse.is_contiguous():
+            raise ValueError(f"lse must be contiguous float32 {list(self.lse_shape)} on {self.device}")
+        return lse
+
+    def workspace(self, backward: bool, given=None):
+        import torch
+
+        out = ctypes.c_size_t(0)
+        _check(load_library().mca_exact_workspace_size(ctypes.byref(self.desc), int(backward), ctypes.byref(out)),
+               "mca_exact_workspace_size")
+        if given is not None and given.numel() * given.element_size() >= out.value:
+            if given.device != self.device or not given.is_contiguous():
+                raise ValueError(f"workspace must be a contiguous tensor on {self.device}")
+            return given
+        return torch.empty(out.value, dtype=torch.uint8, device=self.device) if out.value else None
+
+    def new(self, shape, dtype=None):
+        import torch
+
+        return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
+
+    def on_device(self):
+        import torch
+
+        return torch.cuda.device(self.device)
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def exact_attention_forward(Q, K, V, *, heads: int, kv_heads: Optional[int] = None, scale: Optional[float] = None,
+                            q_lens=None, kv_lens=None, q_pos=None, causal: bool = False, window: int = 0,
+                            bias: Optional[RelativeBias] = None, workspace=None, out=None) -> ExactResult:
+    """Exact attention Y = softmax(scale Q K^T + bias) V per head, and the row log-sum-exp, on the
+    current HIP stream of Q's device.
+
+    Q: [B, n_q, heads*64]; K, V: [B, n_k, kv_heads*64] (``kv_heads`` divides ``heads``; default: all);
+    all float32 or all bfloat16 on one device, columns contiguous, rows and batch at any strides
+    of whole 16 bytes (slices of one projected tensor, a cache longer than what is used).
+    ``scale``: 1/8 by default. q_lens, kv_lens: optional int32 [B], valid rows (padded queries give
+    0, padded keys are not read). q_pos: optional int32 [B], the position of each batch row's first
+    query: for a few new tokens behind a cached prefix, kv_lens - n_q. ``causal``: keys up to the
+    query's position. ``window``: 0, or an even local window with a global first token. ``bias``: a
+    RelativeBias. ``out`` may pass preallocated (Y, lse).
+    Returns Y [B, n_q, heads*64] of Q's dtype and lse [B, heads, n_q] float32 (-inf where a query
+    attends no key; its Y is 0).
+    """
+    import torch
+
+    lib = load_library()
+    call = _ExactCall(Q, K, V, heads, kv_heads, scale, q_lens, kv_lens, q_pos, causal, window, bias)
+    ws = call.workspace(False, workspace)
+    Y, lse = out if out is not None else (call.new(call.q_shape), call.new(call.lse_shape, torch.float32))
+    y = call.rows("Y", Y, call.q_shape)
+    call.check_lse(lse)
+    with call.on_device():
+        _check(lib.mca_exact_attention_forward(call.desc, call.q, call.k, call.v, y, _ptr(lse), _ptr(ws), _bytes(ws),
+                                               _stream_handle(call.device)), "mca_exact_attention_forward")
+    return ExactResult(Y, lse)
+
+
+def exact_attention_backward(dY, Q, K, V, Y, lse, *, heads: int, kv_heads: Optional[int] = None,
+                             scale: Optional[float] = None, q_lens=None, kv_lens=None, q_pos=None, causal: bool = False,
+                             window: int = 0, bias: Optional[RelativeBias] = None, workspace=None, out=None) -> ExactGradients:
+    """Gradients of ``exact_attention_forward`` from dY [B, n_q, heads*64]: dQ, dK, dV and, with a
+    bias, its table's gradient, each of Q's dtype, written on the current HIP stream of Q's device.
+    Y and lse are the forward call's results, the other arguments its own. ``out`` may pass
+    preallocated (dQ, dK, dV, dbias or None), at strides of their own."""
+    lib = load_library()
+    call = _ExactCall(Q, K, V, heads, kv_heads, scale, q_lens, kv_lens, q_pos, causal, window, bias)
+    ws = call.workspace(True, workspace)
+    if out is None:
+        out = (call.new(call.q_shape), call.new(call.k_shape), call.new(call.k_shape),
+               None if bias is None else call.new(bias.table.shape))
+    dQ, dK, dV, dbias = out
+    dy, y, dq = (call.rows(n, t, call.q_shape) for n, t in (("dY", dY), ("Y", Y), ("dQ", dQ)))
+    dk, dv = (call.rows(n, t, call.k_shape) for n, t in (("dK", dK), ("dV", dV)))
+    call.check_lse(lse)
+    if (bias is None) != (dbias is None) or dbias is not None and (
+            dbias.shape != bias.table.shape or dbias.dtype != Q.dtype or dbias.device != Q.device or not dbias.is_contiguous()):
+        raise ValueError("dbias must have the bias table's shape, dtype and device (None without a bias)")
+    with call.on_device():
+        _check(lib.mca_exact_attention_backward(call.desc, dy, call.q, call.k, call.v, y, _ptr(lse), dq, dk, dv, _ptr(dbias),
+                                                _ptr(ws), _bytes(ws), _stream_handle(call.device)),
+               "mca_exact_attention_backward")
+    return ExactGradients(dQ, dK, dV, dbias)
+
+
+class ExactPlan:
+    """Exact attention with every argument but the stream bound once, so that ``forward()`` and, with
+    a dY, ``backward()`` are single C calls: for training loops on fixed buffers and for serving.
+    Results are in Y, lse and dQ, dK, dV, dbias, overwritten by each call. One plan's calls share its
+    workspace: calls that overlap in time (streams, replayed graphs) need plans of their own."""
+
+    def __init__(self, Q, K, V, dY=None, *, heads: int, kv_heads: Optional[int] = None, scale: Optional[float] = None,
+                 q_lens=None, kv_lens=None, q_pos=None, causal: bool = False, window: int = 0,
+                 bias: Optional[RelativeBias] = None):
+        import torch
+
+        lib = load_library()
+        c = self._call = _ExactCall(Q, K, V, heads, kv_heads, scale, q_lens, kv_lens, q_pos, causal, window, bias)
+        self.Y, self.lse = c.new(c.q_shape), c.new(c.lse_shape, torch.float32)
+        self.dQ = self.dK = self.dV = self.dbias = None
+        y = c.rows("Y", self.Y, c.q_shape)
+        ws = c.workspace(False)
+        self._forward = (lib.mca_exact_attention_forward, "mca_exact_attention_forward",
+                         tuple(ctypes.byref(x) for x in (c.desc, c.q, c.k, c.v, y)) + (_ptr(self.lse), _ptr(ws), _bytes(ws)))
+        self._backward = None
+        self._keep = [dY, ws, y]
+        if dY is not None:
+            self.dQ, self.dK, self.dV = c.new(c.q_shape), c.new(c.k_shape), c.new(c.k_shape)
+            self.dbias = None if bias is None else c.new(bias.table.shape)
+            rows = [c.rows("dY", dY, c.q_shape), c.q, c.k, c.v, y]
+            grads = [c.rows("dQ", self.dQ, c.q_shape), c.rows("dK", self.dK, c.k_shape), c.rows("dV", self.dV, c.k_shape)]
+            wb = c.workspace(True)
+            self._keep += [wb, rows, grads]
+            self._backward = (lib.mca_exact_attention_backward, "mca_exact_attention_backward",
+                              tuple(ctypes.byref(x) for x in [c.desc] + rows) + (_ptr(self.lse),) +
+                              tuple(ctypes.byref(x) for x in grads) + (_ptr(self.dbias), _ptr(wb), _bytes(wb)))
+        self._current_device, self._index = torch.cuda.current_device, c.device.index
+
+    def _run(self, bound):
+        fn, name, args = bound
+        if self._current_device() != self._index:
+            with self._call.on_device():
+                st = fn(*args, _stream_handle(self._call.device))
+        else:
+            st = fn(*args, _stream_handle(self._call.device))
+        if st != MCA_OK:
+            _check(st, name)
+
+    def forward(self):
+        self._run(self._forward)
+
+    def backward(self):
+        if self._backward is None:
+            raise ValueError("the plan was made without dY")
+        self._run(self._backward)

@@ -23,7 +23,8 @@ LIB = os.path.join(PKG, "libmca.so")
 PROBE_LIB = os.path.join(PKG, "libmca_probe.so")
 ARCH = "gfx950"
 
-SOURCES = ["k_attention.hip", "k_sample.hip", "k_gather.hip", "k_prepare.hip", "mca_api.cpp"]
+SOURCES = ["k_attention.hip", "k_sample.hip", "k_gather.hip", "k_prepare.hip", "k_exact_forward.hip",
+           "k_exact_backward.hip", "mca_api.cpp", "exact_api.cpp"]
 PROBE_SOURCES = ["issue_probe.hip"]
 
 CXXFLAGS = [

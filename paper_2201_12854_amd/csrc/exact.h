@@ -1,0 +1,59 @@
+// Host-side launch interface of the exact attention kernels (internal to libmca).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace mca {
+
+constexpr int kMaxBuckets = 128;       // rows of the relative bias table
+constexpr int kMaxBiasDistance = 256;  // distances from here on share the last bucket
+
+// Rows of a [batch, rows, heads * 64] tensor: strides in elements, heads and columns contiguous.
+struct ExactRows {
+  const void* data;
+  int64_t batch, row;
+};
+struct ExactOut {
+  void* data;
+  int64_t batch, row;
+};
+
+struct ExactParams {
+  int B, nq, nk, H, Hk;
+  int G;                      // query heads per key head
+  int Gp;                     // heads that the kernels of 32 rows put side by side (1 or G)
+  int causal, window, half;   // window: 0 none, else |p - j| <= half, or p = 0, or j = 0
+  int bf16;
+  float scale, s2;            // s2 = scale log2(e)
+  const int32_t *q_lens, *kv_lens, *q_pos;  // [B] or null
+  ExactRows Q, K, V, Y, dY;
+  ExactOut Yo, dQ, dK, dV;
+  float* lse;                 // [B, H, nq], natural logarithm
+  // relative bias
+  const void* table;          // [buckets, H] or null
+  void* dtable;
+  int buckets, side;          // side: buckets of one direction (all of them if not bidirectional)
+  int bidirectional, E, D;    // distances below E have a bucket each, those from D on the last one
+  int nthr;                   // distances from thr[k] on are in bucket E + 1 + k or a later one
+  int thr[kMaxBuckets / 2];
+  // workspace
+  int splits;                 // forward: parts of the keys that blocks of their own take
+  float* part_y;              // [splits][rows of 32][64] sums of P V under the part's maximum
+  float2* part_ml;            // [splits][rows of 32] that maximum (base-2 units) and the sum of P
+  float2* rowstat;            // backward: [B, H, nq] (log-sum-exp in base-2 units, dY . Y)
+  float* part_bias;           // backward: [parts][buckets][H] gradient of a block of rows
+  int bias_parts;
+};
+
+inline int exact_bias_entries(int D) { return 2 * D + 129; }  // rel = j - p in [-D - 64, D + 64]
+// Rows (query, head) that the kernels of 32 rows pad to.
+inline int64_t exact_row_tiles(int64_t nq, int64_t Gp) { return (nq * Gp + 31) / 32; }
+
+int exact_splits(const ExactParams& p);
+int exact_group(const ExactParams& p, bool backward);  // Gp
+hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s);
+hipError_t launch_exact_backward(const ExactParams& p, hipStream_t s);
+
+}  // namespace mca

@@ -12,10 +12,13 @@
 
 #include "mca.h"
 #include "mca_kernels.h"
+#include "mca_status.h"
 
 namespace {
-
 thread_local char g_last_error[512] = "";
+}
+
+namespace mca {
 
 mca_status fail(mca_status st, const char* fmt, ...) {
   va_list ap;
@@ -30,13 +33,18 @@ mca_status ok() {
   return MCA_OK;
 }
 
+}  // namespace mca
+
+namespace {
+
+using mca::aligned16;
+using mca::align256;
+using mca::fail;
+using mca::ok;
+
 constexpr int64_t kMaxDin = 2048;
 constexpr int64_t kMaxDout = 2048;
 constexpr int64_t kMaxTokens = int64_t(1) << 30;
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-size_t align256(size_t v) { return (v + 255) & ~size_t(255); }
 
 struct Layout {
   size_t colmax_part, row_c, henc, list, ucount, acol, total;
