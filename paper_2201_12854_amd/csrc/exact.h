@@ -42,9 +42,11 @@ struct ExactParams {
   int splits;                 // forward: parts of the keys that blocks of their own take
   float* part_y;              // [splits][rows of 32][64] sums of P V under the part's maximum
   float2* part_ml;            // [splits][rows of 32] that maximum (base-2 units) and the sum of P
-  float2* rowstat;            // backward: [B, H, nq] (log-sum-exp in base-2 units, dY . Y)
-  float* part_bias;           // backward: [parts][buckets][H] gradient of a block of rows
-  int bias_parts;
+  float* rowstat;             // backward: two planes [B, H, nq] that k_exact_dkv starts from: of a row with
+                              // c = log2(e) log-sum-exp (infinity without keys) and D = dY . Y, float32
+                              // c and D, bf16 -c / s2 and -D (where its accumulators start)
+  float* part_bias;           // backward: [parts][buckets][H] gradient of a wave's or block's rows
+  int bias_parts;             // exact_bias_parts
 };
 
 inline int exact_bias_entries(int D) { return 2 * D + 129; }  // rel = j - p in [-D - 64, D + 64]
@@ -52,6 +54,7 @@ inline int exact_bias_entries(int D) { return 2 * D + 129; }  // rel = j - p in 
 inline int64_t exact_row_tiles(int64_t nq, int64_t Gp) { return (nq * Gp + 31) / 32; }
 
 int exact_splits(const ExactParams& p);
+int exact_bias_parts(const ExactParams& p);  // blocks of rows that give the bias gradient a part each
 int exact_group(const ExactParams& p, bool backward);  // Gp
 hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s);
 hipError_t launch_exact_backward(const ExactParams& p, hipStream_t s);

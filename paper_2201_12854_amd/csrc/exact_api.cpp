@@ -151,7 +151,7 @@ ExactParams params_of(const mca_exact_desc& d, bool backward) {
   if (p.table) set_buckets(p, d.bias_buckets, d.bias_max_distance, d.bias_bidirectional);
   p.Gp = mca::exact_group(p, backward);
   p.splits = backward ? 1 : mca::exact_splits(p);
-  p.bias_parts = (int)(p.B * mca::exact_row_tiles(p.nq, p.Gp));
+  p.bias_parts = backward ? mca::exact_bias_parts(p) : 0;
   return p;
 }
 
@@ -164,7 +164,7 @@ size_t carve(ExactParams& p, bool backward, char* ws) {
     return at;
   };
   if (backward) {
-    p.rowstat = reinterpret_cast<float2*>(take(sizeof(float2) * (size_t)p.B * p.H * p.nq));
+    p.rowstat = reinterpret_cast<float*>(take(8 * (size_t)p.B * p.H * p.nq));
     if (p.table) p.part_bias = reinterpret_cast<float*>(take(4 * (size_t)p.bias_parts * p.buckets * p.H));
   } else if (p.splits > 1) {
     const size_t rows = (size_t)p.splits * p.B * (p.H / p.Gp) * mca::exact_row_tiles(p.nq, p.Gp) * 32;

@@ -176,6 +176,113 @@ __device__ __forceinline__ void ex_cols_product(f32x16_t (&y)[2], const char* ti
   }
 }
 
+// ------------------------------------------------------------------ bf16 tiles of 64 rows
+// Shared by a block of four waves and loaded by all of them: wave w takes rows 8 w .. 8 w + 7 and
+// those 32 further. Offset of a lane's 16 bytes in memory for a row pitch, and the operands.
+constexpr int kTile64 = 64 * 128;  // bytes
+
+// COLS: a tile that is read by columns only, with a permutation of period 4.
+__device__ __forceinline__ int ex_swz_cols(int r) { return ((r & 1) << 1) | ((r & 2) << 1); }
+template <bool COLS = false>
+__device__ __forceinline__ uint32_t ex_load64(int wave, int lane, int pitch) {
+  const int row = 8 * wave + (lane >> 3);
+  return (uint32_t)(row * pitch + (((lane & 7) ^ (COLS ? ex_swz_cols(row) : ex_swz<uint16_t>(row))) << 4));
+}
+__device__ __forceinline__ void ex_load_tile64(const char* base, int pitch, int row0, int limit, uint32_t off, uint32_t lds,
+                                               int wave) {
+  ex_load_lds16(ex_rsrc(base, pitch, row0, limit, 128), off, lds + 1024u * wave);
+  ex_load_lds16(ex_rsrc(base, pitch, row0 + 32, limit, 128), off, lds + 4096u + 1024u * wave);
+}
+
+// The lane's byte addresses in a tile: row c, chunks 2 g + hf; and the transposing reads of rows
+// 4 hf + (lane % 16) / 4, columns 32 cc ... (rows 8 further: col8, which a COLS tile does not need).
+template <bool COLS>
+struct ExCols64 {
+  int col[2], col8[COLS ? 1 : 2];
+};
+struct ExRows64 {
+  int row[4];
+};
+__device__ __forceinline__ ExRows64 ex_rows64(int lane) {
+  ExRows64 a;
+  const int c = lane & 31, hf = lane >> 5;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) a.row[g] = c * 128 + (((2 * g + hf) ^ ex_swz<uint16_t>(c)) << 4);
+  return a;
+}
+template <bool COLS>
+__device__ __forceinline__ ExCols64<COLS> ex_cols64(int lane) {
+  ExCols64<COLS> a;
+  const int hf = lane >> 5, i16 = lane & 15, row = 4 * hf + (i16 >> 2);
+#pragma unroll
+  for (int cc = 0; cc < 2; ++cc) {
+    const int col = 32 * cc + 16 * ((lane >> 4) & 1) + 4 * (i16 & 3);
+    auto at = [&](int r) { return r * 128 + (((col >> 3) ^ (COLS ? ex_swz_cols(r) : ex_swz<uint16_t>(r))) << 4) + (col & 7) * 2; };
+    a.col[cc] = at(row);
+    if constexpr (!COLS) a.col8[cc] = at(row + 8);
+  }
+  return a;
+}
+__device__ __forceinline__ u32x4_t ex_read_row(const char* tile, const ExRows64& a, int half, int g) {
+  return *reinterpret_cast<const u32x4_t*>(tile + a.row[g] + half * 4096);
+}
+// Rows 32 half + 16 pp .. + 15 of columns 32 cc .. as the first operand of a product over rows.
+template <bool COLS>
+__device__ __forceinline__ u32x4_t ex_read_col(const char* tile, const ExCols64<COLS>& a, int half, int pp, int cc) {
+  typedef short v4i16 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+  const int o = half * 4096 + pp * 2048, o8 = COLS ? a.col[cc] + 1024 : a.col8[COLS ? 0 : cc];
+  const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(tile + a.col[cc] + o)));
+  const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(tile + o8 + o)));
+  return u32x4_t{lo.x, lo.y, hi.x, hi.y};
+}
+
+// 32 rows of 64 sums, y[cc][r] = column 32 cc + 8 (r / 4) + 4 hf + r % 4 of row c, times `scale`, to
+// bf16 rows in memory: through LDS (`st`, 32 x 144 bytes of the wave's own), so that eight lanes
+// write a whole row. Rows r >= rows are left out.
+__device__ __forceinline__ void ex_store_rows32(char* st, const f32x16_t (&y)[2], float scale, char* out, int64_t pitch,
+                                                int rows, int lane) {
+  const int c = lane & 31, hf = lane >> 5;
+#pragma unroll
+  for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4)
+      *reinterpret_cast<uint2*>(st + c * 144 + 64 * cc + 16 * (r >> 2) + 8 * hf) =
+          make_uint2(pack_bf16x2(y[cc][r] * scale, y[cc][r + 1] * scale), pack_bf16x2(y[cc][r + 2] * scale, y[cc][r + 3] * scale));
+  wave_lds_sync();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int row = 8 * k + (lane >> 3);
+    const uint4 v = *reinterpret_cast<const uint4*>(st + row * 144 + 16 * (lane & 7));
+    if (row < rows) *reinterpret_cast<uint4*>(out + row * pitch + 16 * (lane & 7)) = v;
+  }
+  wave_lds_sync();
+}
+
+// Keeps the computation of x before this point and what follows behind it.
+template <typename T>
+__device__ __forceinline__ void ex_pin(T& x) { asm volatile("" : "+v"(x)); }
+
+// x, which the compiler can neither foresee nor move: what a rare branch computes from it is not kept
+// in registers outside of the branch.
+__device__ __forceinline__ int ex_opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The rows tile `qt` and (batch row, head) `pair` of block `bid`: the tiles of a pair on one XCD where
+// the pairs come in eights.
+__device__ __forceinline__ void ex_block_pair(int bid, int tiles, int pairs, int& qt, int& pair) {
+  if (pairs % 8 == 0) {
+    const int G = 8 * tiles, w = bid % G;
+    pair = bid / G * 8 + w % 8;
+    qt = w / 8;
+  } else {
+    pair = bid / tiles;
+    qt = bid % tiles;
+  }
+}
+
 // ------------------------------------------------------------------ lanes
 // The value of the other half's lane (l ^ 32).
 __device__ __forceinline__ float ex_other_half(float v) {
@@ -230,27 +337,29 @@ __device__ __forceinline__ ExSpan ex_queries_of(const ExactParams& p, const ExRo
   return ex_span(lo, hi, extra);
 }
 
-// The tiles of 32 that a block visits: an extra one first (the global key or query of a window), then
-// lo .. hi. `n` of them.
+// The tiles (of 32 or 64 rows) that a block visits: an extra one first (the global key or query of a
+// window), then lo .. hi. `n` of them.
 struct ExTiles {
   int first, lo, n;  // first < 0: none
 };
 __device__ __forceinline__ int ex_tile_at(const ExTiles& t, int i) {
   return t.first >= 0 ? (i == 0 ? t.first : t.lo + i - 1) : t.lo + i;
 }
+template <int TILE>
 __device__ __forceinline__ ExTiles ex_tiles(int lo, int hi, int extra) {  // of elements
   ExTiles t{-1, 0, 0};
   if (hi >= lo) {
-    t.lo = lo / 32;
-    t.n = hi / 32 - t.lo + 1;
+    t.lo = lo / TILE;
+    t.n = hi / TILE - t.lo + 1;
   }
-  if (extra >= 0 && (t.n == 0 || extra / 32 < t.lo || extra / 32 >= t.lo + t.n)) {
-    t.first = extra / 32;
+  if (extra >= 0 && (t.n == 0 || extra / TILE < t.lo || extra / TILE >= t.lo + t.n)) {
+    t.first = extra / TILE;
     t.n += 1;
   }
   return t;
 }
 // Key tiles of the queries at positions pmin .. pmax.
+template <int TILE = 32>
 __device__ __forceinline__ ExTiles ex_key_tiles(const ExactParams& p, int pmin, int pmax, int klen) {
   int lo = 0, hi = klen - 1, extra = -1;
   if (p.causal) hi = min(hi, pmax);
@@ -259,9 +368,10 @@ __device__ __forceinline__ ExTiles ex_key_tiles(const ExactParams& p, int pmin, 
     hi = min(hi, pmax + p.half);
     if (klen > 0 && (!p.causal || pmax >= 0)) extra = 0;
   }
-  return ex_tiles(lo, hi, extra);
+  return ex_tiles<TILE>(lo, hi, extra);
 }
 // Query tiles of the keys jmin .. jmax (jmax < klen).
+template <int TILE = 32>
 __device__ __forceinline__ ExTiles ex_query_tiles(const ExactParams& p, const ExRow0& r, int jmin, int jmax) {
   int lo = 0, hi = r.qlen - 1, extra = -1;
   if (jmax < jmin) return ExTiles{-1, 0, 0};
@@ -271,7 +381,7 @@ __device__ __forceinline__ ExTiles ex_query_tiles(const ExactParams& p, const Ex
     hi = min(hi, jmax + p.half - r.pos);
     if (!p.causal && -r.pos >= 0 && -r.pos < r.qlen) extra = -r.pos;
   }
-  return ex_tiles(lo, hi, extra);
+  return ex_tiles<TILE>(lo, hi, extra);
 }
 // Whether every query at pmin .. pmax attends every key of k0 .. k0 + 31.
 __device__ __forceinline__ bool ex_whole(const ExactParams& p, int pmin, int pmax, int k0, int klen) {

@@ -6,13 +6,14 @@
 // k_exact_dkv (per keys, over the query heads that share them). That takes S and dP twice: seven
 // products for the five that the formulas need.
 #include "exact_device.h"
+#include "mca_kernels.h"
 
 namespace mca {
 namespace {
 
 template <typename T> constexpr int kBwdStages = ExFmt<T>::ES == 2 ? 3 : 2;
 template <typename T> constexpr int kDqLds = kExWaves * kBwdStages<T> * 2 * tile_bytes<T>();
-template <typename T> constexpr int kDkvStage = 2 * tile_bytes<T>() + 256;  // Q, dY, 32 row statistics
+template <typename T> constexpr int kDkvStage = 2 * tile_bytes<T>() + 512;  // Q, dY, two planes of statistics
 template <typename T> constexpr int kDkvLds = kExWaves * kBwdStages<T> * kDkvStage<T>;
 constexpr int kYS = kDHead + 4;  // row pitch of the sums that the waves of a block join in LDS
 
@@ -45,23 +46,90 @@ __device__ __forceinline__ void ex_join_sums(float (&o)[8], const float* ys, int
   }
 }
 
+// What k_exact_dkv starts from.
+template <typename T>
+__device__ __forceinline__ void ex_put_stat(const ExactParams& p, int64_t row, float c, float D) {
+  const int64_t plane = (int64_t)p.B * p.H * p.nq;
+  p.rowstat[row] = ExFmt<T>::ES == 2 ? -c * (1.f / p.s2) : c;
+  p.rowstat[plane + row] = ExFmt<T>::ES == 2 ? -D : D;
+}
+
+// ------------------------------------------------------------------ sums along diagonals
+// Adds the 63 diagonals of a 32x32 tile (lane: query row c; register r: key (r & 3) + 8 (r >> 2) + 4 hf)
+// to at[0 .. 62], diagonal key - query + 31. Row c goes to LDS shifted by its number, 64 floats to
+// a row, so that a diagonal is a column; then a lane adds two columns over half of the rows. The
+// entries that a row leaves are zeros: written here (FILL), or once by the caller, as every tile
+// leaves the same ones.
+template <bool FILL>
+__device__ __forceinline__ void ex_diagonals(float* st, const f32x16_t& x, float* at, int lane) {
+  const int c = lane & 31, hf = lane >> 5;
+  wave_lds_sync();
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int e = (r & 3) + 8 * (r >> 2) + 4 * hf + 31 - c;
+    st[c * 64 + e] = x[r];
+    if (FILL) st[c * 64 + ((e + 32) & 63)] = 0.f;
+  }
+  wave_lds_sync();
+  float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const float2 v = *reinterpret_cast<const float2*>(st + (16 * hf + k) * 64 + 2 * c);
+    a0 += v.x;
+    a1 += v.y;
+  }
+  // lanes below 32 take column 2 c, the others 2 c + 1, of both halves of the rows
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(a0), __float_as_uint(a1), false, false);
+  float* o = at + 2 * c + hf;
+  *o += __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  wave_lds_sync();
+}
+// A lane's sums of far tiles: to entries of the far sides that no other lane uses.
+__device__ __forceinline__ void ex_add_far(float* dg, int n, float left, float right, int lane) {
+  wave_lds_sync();
+  left += ex_other_half(left);
+  right += ex_other_half(right);
+  if (lane < 32) {
+    dg[lane] += left;
+    dg[n - 1 - lane] += right;
+  }
+}
+// A part of the bias gradient: t holds the entries of one head. A bucket's entries are neighbours.
+__device__ __forceinline__ void ex_put_buckets(const ExactParams& p, const float* t, int64_t part, int head) {
+  const int far = p.D + 64;
+  for (int k = threadIdx.x; k < p.buckets; k += kExThreads) {
+    const int kk = k % p.side;
+    const bool right = k >= p.side;
+    int lo = kk, hi = kk;  // distances
+    if (kk >= p.E) {
+      lo = kk == p.E ? p.E : p.thr[kk - p.E - 1];
+      hi = kk - p.E < p.nthr ? p.thr[kk - p.E] - 1 : far;
+    }
+    const int a = right ? max(lo, 1) : -hi;
+    const int z = right ? hi : !p.bidirectional && kk == 0 ? far : -lo;  // keys ahead share bucket 0
+    float sum = 0.f;
+    for (int r = a; r <= z; ++r) sum += t[far + r];
+    p.part_bias[(part * p.buckets + k) * p.H + head] = sum;
+  }
+}
+
 // ------------------------------------------------------------------ dQ
 // Blocks of 32 (query, head) rows whose key tiles the four waves share, as k_exact_rows. S^T = K Q^T
 // and dP^T = V dY^T: the row's c and D are one value per lane, and dS feeds dQ^T = K^T dS^T.
 //
-// The bias gradient: a pair's dS belongs to entry rel = j - p, and in one register of a half wave the
-// 32 lanes (one query position each, or another head) hold 32 different entries. Every half wave
-// has an array of its own in LDS, so that no two lanes add to one entry in one instruction and the
-// sums have a fixed order; a tile whose pairs all lie D or further away is summed per lane in a
-// register and added to entries of the far side that no other lane uses.
+// The bias gradient: a pair's dS belongs to the diagonal rel = j - p of its tile. A tile whose pairs all
+// lie D or further away is summed per lane in a register. The 63 diagonals of another tile are
+// summed through LDS (ex_diagonals), in the tile's own buffer once the products are done with it,
+// into an array per wave: adding every pair to it with LDS atomics took 130 cycles an instruction
+// (16 x 512 tokens, 12 heads: 306 us against 117 for k_exact_dkv).
 template <typename T, bool BIAS>
 __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
   extern __shared__ __align__(16) char smem[];
   constexpr int ES = ExFmt<T>::ES, ST = kBwdStages<T>, TB = tile_bytes<T>();
   const int n = 2 * p.D + 129;
-  float* tb = reinterpret_cast<float*>(smem + kDqLds<T>);  // [Gp][n]
-  float* dg = tb + p.Gp * n;                               // [wave][half][Gp][n]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float* tb = reinterpret_cast<float*>(smem + kDqLds<T>);  // with a bias Gp = 1: one head's table
+  float* dg = tb + n + wave * n;                           // the wave's sums per entry
   const int c = lane & 31, hf = lane >> 5;
   const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp;
   int bid = blockIdx.x;
@@ -113,18 +181,16 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
     cr = lse == -INFINITY ? INFINITY : lse * kLog2e;
   }
   D += ex_other_half(D);
-  if (wave == 0 && hf == 0 && i < p.nq) p.rowstat[((int64_t)b * p.H + head) * p.nq + i] = make_float2(cr, D);
+  if (wave == 0 && hf == 0 && i < p.nq) ex_put_stat<T>(p, ((int64_t)b * p.H + head) * p.nq + i, cr, D);
   const int pos = br.pos + i;
   const ExSpan keys = ex_keys_of(p, pos, br.klen);
   const float* tl = nullptr;
-  float* dl = nullptr;
   float far_l = 0.f, far_r = 0.f;
   if constexpr (BIAS) {
-    ex_fill_bias<T>(p, tb, hx * p.Gp, p.Gp);
-    for (int e = threadIdx.x; e < 2 * kExWaves * p.Gp * n; e += kExThreads) dg[e] = 0.f;
+    ex_fill_bias<T>(p, tb, head, 1);
+    for (int e = lane; e < n; e += 64) dg[e] = 0.f;
     __syncthreads();
-    tl = tb + g * n + p.D + 64;
-    dl = dg + ((2 * wave + hf) * p.Gp + g) * n + p.D + 64;
+    tl = tb + p.D + 64;
   }
   f32x16_t dq[2] = {ex_zero16(), ex_zero16()};
 
@@ -134,7 +200,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
     load(idx + (ST - 1) * kExWaves, slot == 0 ? ST - 1 : slot - 1);
     wait_vmcnt<(ST - 1) * 2 * ExFmt<T>::NL>();
     asm volatile("" ::: "memory");
-    const char* kt = smem + (wave * ST + slot) * 2 * TB;
+    char* kt = smem + (wave * ST + slot) * 2 * TB;
     const int k0 = ex_tile_at(tiles, idx) * 32;
     f32x16_t x = ex_rows_product<T>(kt, q, c, hf);
     const f32x16_t dp = ex_rows_product<T>(kt + TB, dy, c, hf);
@@ -160,6 +226,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) x[r] = ex_exp2(x[r]) * (dp[r] - D);
+    ex_cols_product<T>(dq, kt, x, lane);
     if constexpr (BIAS) {
       if (side != 0) {
         float sum = 0.f;
@@ -168,27 +235,20 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
         far_l += side < 0 ? sum : 0.f;
         far_r += side > 0 ? sum : 0.f;
       } else {
-        float* at = dl + (k0 + 4 * hf - pos);
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          __hip_atomic_fetch_add(at + (r & 3) + 8 * (r >> 2), x[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        ex_diagonals<true>(reinterpret_cast<float*>(kt), x, dg + p.D + 33 + k0 - pmin, lane);
       }
     }
-    ex_cols_product<T>(dq, kt, x, lane);
     slot = slot == ST - 1 ? 0 : slot + 1;
   }
-  if constexpr (BIAS) {
-    __hip_atomic_fetch_add(dl - p.D - 64 + c, far_l, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    __hip_atomic_fetch_add(dl + p.D + 64 - c, far_r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-  }
+  if constexpr (BIAS) ex_add_far(dg, n, far_l, far_r, lane);
   wait_vmcnt<0>();  // no load is under way into what is written next
   __syncthreads();
   float* ys = reinterpret_cast<float*>(smem);
   ex_put_sums(ys, dq, wave * 32 + c, hf);
   if constexpr (BIAS) {
-    for (int e = threadIdx.x; e < p.Gp * n; e += kExThreads) {  // the half waves' arrays
-      float t = dg[e];
-      for (int k = 1; k < 2 * kExWaves; ++k) t += dg[k * p.Gp * n + e];
+    for (int e = threadIdx.x; e < n; e += kExThreads) {
+      float t = tb[n + e];
+      for (int k = 1; k < kExWaves; ++k) t += tb[(1 + k) * n + e];
       tb[e] = t;
     }
   }
@@ -201,24 +261,21 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
     ex_store8(static_cast<T*>(p.dQ.data) + b * p.dQ.batch + ir * p.dQ.row + (hx * p.Gp + vr % p.Gp) * kDHead + col, o);
   }
   if constexpr (BIAS) {
-    // a bucket's entries are neighbours: distances lo .. hi of its side
-    for (int e = threadIdx.x; e < p.Gp * p.buckets; e += kExThreads) {
-      const int gg = e / p.buckets, k = e % p.buckets, kk = k % p.side;
-      const bool right = k >= p.side;
-      const int far = p.D + 64;
-      int lo = kk, hi = kk;
-      if (kk >= p.E) {
-        lo = kk == p.E ? p.E : p.thr[kk - p.E - 1];
-        hi = kk - p.E < p.nthr ? p.thr[kk - p.E] - 1 : far;
-      }
-      int a = right ? max(lo, 1) : -hi, z = right ? hi : -lo;  // rel a .. z
-      if (!p.bidirectional && kk == 0) z = far;                // keys behind the query
-      const float* t = tb + gg * n + far;
-      float sum = 0.f;
-      for (int r = a; r <= z; ++r) sum += t[r];
-      p.part_bias[((int64_t)(b * nvt + vt) * p.buckets + k) * p.H + hx * p.Gp + gg] = sum;
-    }
+    ex_put_buckets(p, tb, b * nvt + vt, head);
   }
+}
+
+// Sums a (bucket, head)'s parts: entry e = bucket * H + head, by the lanes of a wave.
+template <typename T>
+__device__ __forceinline__ void ex_sum_bias(const ExactParams& p, int e, int lane) {
+  if (e >= p.buckets * p.H) return;
+  float sum = 0.f;
+  for (int k = lane; k < p.bias_parts; k += 64) sum += p.part_bias[(int64_t)k * p.buckets * p.H + e];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if (lane != 0) return;
+  if constexpr (ExFmt<T>::ES == 2) static_cast<T*>(p.dtable)[e] = (T)f32_to_bf16_bits(sum);
+  else static_cast<T*>(p.dtable)[e] = sum;
 }
 
 // ------------------------------------------------------------------ dK, dV
@@ -234,16 +291,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
   const int nkt = (p.nk + 31) / 32;
   int bid = blockIdx.x;
   if (BIAS && bid >= nkt * p.Hk * p.B) {
-    const int e = (bid - nkt * p.Hk * p.B) * kExWaves + wave;  // bucket * H + head
-    if (e >= p.buckets * p.H) return;
-    float sum = 0.f;
-    for (int k = lane; k < p.bias_parts; k += 64) sum += p.part_bias[(int64_t)k * p.buckets * p.H + e];
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    if (lane == 0) {
-      if constexpr (ES == 2) static_cast<T*>(p.dtable)[e] = (T)f32_to_bf16_bits(sum);
-      else static_cast<T*>(p.dtable)[e] = sum;
-    }
+    ex_sum_bias<T>(p, (bid - nkt * p.Hk * p.B) * kExWaves + wave, lane);
     return;
   }
   const int c = lane & 31, hf = lane >> 5, n = 2 * p.D + 129;
@@ -280,8 +328,9 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
       const uint32_t to = lds + slot * SB;
       ex_load_tile<T>(ex_rsrc(Qb, p.Q.row * ES, i0, limit, ExFmt<T>::RB), (int)p.Q.row * ES, to, lane);
       ex_load_tile<T>(ex_rsrc(Yb, p.dY.row * ES, i0, limit, ExFmt<T>::RB), (int)p.dY.row * ES, to + TB, lane);
-      ex_load_lds4(ex_rsrc(reinterpret_cast<const char*>(p.rowstat + ((int64_t)b * p.H + h) * p.nq), 8, i0, limit, 8),
-                   lane * 4, to + 2 * TB);
+      const char* st = reinterpret_cast<const char*>(p.rowstat + ((int64_t)b * p.H + h) * p.nq);
+      ex_load_lds4(ex_rsrc(st, 4, i0, limit, 4), lane * 4, to + 2 * TB);
+      ex_load_lds4(ex_rsrc(st + 4 * (int64_t)p.B * p.H * p.nq, 4, i0, limit, 4), lane * 4, to + 2 * TB + 256);
     };
 #pragma unroll
     for (int k = 0; k < ST - 1; ++k) load(wave + k * kExWaves, k);
@@ -289,7 +338,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
     for (int idx = wave; idx < total; idx += kExWaves) {
       wait_lds();  // the tile read last is overwritten by the next loads
       load(idx + (ST - 1) * kExWaves, slot == 0 ? ST - 1 : slot - 1);
-      wait_vmcnt<(ST - 1) * (2 * ExFmt<T>::NL + 1)>();
+      wait_vmcnt<(ST - 1) * (2 * ExFmt<T>::NL + 2)>();
       asm volatile("" ::: "memory");
       const char* qt = smem + (wave * ST + slot) * SB;
       const float* stat = reinterpret_cast<const float*>(qt + 2 * TB);
@@ -298,9 +347,19 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
       f32x16_t ds = ex_rows_product<T>(qt + TB, vf, c, hf);
       float cr[16], D[16];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {  // rows 8 (k / 2) + 4 hf + 2 (k % 2), + 1
-        const float4 t = *reinterpret_cast<const float4*>(stat + 2 * (8 * (k >> 1) + 4 * hf + 2 * (k & 1)));
-        cr[2 * k] = t.x, D[2 * k] = t.y, cr[2 * k + 1] = t.z, D[2 * k + 1] = t.w;
+      for (int k = 0; k < 4; ++k) {  // rows 8 k + 4 hf ..
+        const float4 t = *reinterpret_cast<const float4*>(stat + 8 * k + 4 * hf);
+        const float4 u = *reinterpret_cast<const float4*>(stat + 64 + 8 * k + 4 * hf);
+        cr[4 * k] = t.x, cr[4 * k + 1] = t.y, cr[4 * k + 2] = t.z, cr[4 * k + 3] = t.w;
+        D[4 * k] = u.x, D[4 * k + 1] = u.y, D[4 * k + 2] = u.z, D[4 * k + 3] = u.w;
+      }
+      if constexpr (ES == 2) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          x[r] += cr[r];
+          ds[r] += D[r];
+          cr[r] = D[r] = 0.f;
+        }
       }
       if constexpr (BIAS) {
         const float* tl = tb + (idx / tiles.n) * n + p.D + 64;
@@ -348,31 +407,468 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
   ex_store8(static_cast<T*>(p.dV.data) + b * p.dV.batch + jr * p.dV.row + hk * kDHead + col, o);
 }
 
+// ------------------------------------------------------------------ tiles of 64 rows, bf16
+// For grids that fill the card: blocks of 128 rows, four waves of 32, that share the tiles they loop
+// over, loaded straight into LDS two tiles ahead of their use (three buffers). Both kernels are
+// software pipelined by half tiles of 32: a step has the matrix products of S and dP of half tile
+// h + 1 in eight slots, each one MFMA beside the vector work of two pairs of h (P and dS), then the
+// products that P and dS of h feed. The source fixes the order; an operand is read from LDS
+// kAhead slots before its MFMA.
+constexpr int kAhead = 4;
+
+// One MFMA slot's vector work: pairs 2 j, 2 j + 1 of a half tile. The exp2 results of one slot are used
+// in the next.
+struct ExPair {
+  float e0, e1;
+};
+template <bool FMA>  // FMA: a logit is fac * s + add, else fac * s
+__device__ __forceinline__ ExPair ex_pair(const f32x16_t& s, int j, float fac, float add) {
+  ExPair r;
+  const float x0 = FMA ? __fmaf_rn(s[2 * j], fac, add) : s[2 * j] * fac;
+  const float x1 = FMA ? __fmaf_rn(s[2 * j + 1], fac, add) : s[2 * j + 1] * fac;
+  r.e0 = ex_exp2(x0);
+  r.e1 = ex_exp2(x1);
+  ex_pin(r.e0);
+  ex_pin(r.e1);
+  return r;
+}
+
+template <bool BIAS> constexpr int kDqTilesLds = 6 * kTile64 + (BIAS ? kExWaves * 32 * 64 * 4 : 0);
+
+template <bool BIAS>
+__global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_dq_tiles(ExactParams p) {
+  extern __shared__ __align__(16) char smem[];  // three K tiles, three V tiles; diagonals, bias table, its gradient
+  const int n = 2 * p.D + 129;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, hf = lane >> 5;
+  float* st = reinterpret_cast<float*>(smem + 6 * kTile64) + wave * 32 * 64;
+  float* tb = reinterpret_cast<float*>(smem + kDqTilesLds<BIAS>);
+  float* dg = tb + n + wave * n;
+  int qt, pair;
+  const int nqt = (p.nq + 127) / 128;
+  ex_block_pair(blockIdx.x, nqt, p.H * p.B, qt, pair);
+  if (p.causal) qt = nqt - 1 - qt;  // the longest rows first
+  const int h = pair % p.H, b = pair / p.H, hk = h / p.G;
+  const ExRow0 br = ex_batch_row(p, b);
+  const int qw = qt * 128 + wave * 32, i = qw + c;
+  const int last = min(qt * 128 + 128, br.qlen) - 1;
+  const ExTiles tiles = last >= qt * 128 ? ex_key_tiles<64>(p, br.pos + qt * 128, br.pos + last, br.klen) : ExTiles{-1, 0, 0};
+  const int wmin = br.pos + qw, wmax = br.pos + min(qw + 32, br.qlen) - 1;
+
+  const char* Kb = static_cast<const char*>(p.K.data) + (b * p.K.batch + hk * kDHead) * 2;
+  const char* Vb = static_cast<const char*>(p.V.data) + (b * p.V.batch + hk * kDHead) * 2;
+  const int kpitch = (int)p.K.row * 2, vpitch = (int)p.V.row * 2;
+  const uint32_t kl = ex_load64(wave, lane, kpitch), vl = ex_load64(wave, lane, vpitch), lds = lds_addr(smem);
+  auto load = [&](int t, int slot) __attribute__((always_inline)) {  // past the last tile: zeros
+    const int k0 = ex_tile_at(tiles, t) * 64, limit = t < tiles.n ? br.klen : 0;
+    ex_load_tile64(Kb, kpitch, k0, limit, kl, lds + slot * kTile64, wave);
+    ex_load_tile64(Vb, vpitch, k0, limit, vl, lds + (3 + slot) * kTile64, wave);
+  };
+  load(0, 0);
+  const bool live = i < br.qlen;
+  const int64_t hcol = h * kDHead;
+  ExRow<uint16_t> q = ex_zero_row<uint16_t>(), dy = q;
+  float D = 0.f, cr = INFINITY;  // a row without keys, or behind the last query: every P is 0
+  if (live) {
+    q = ex_global_row<uint16_t>(static_cast<const char*>(p.Q.data) + (b * p.Q.batch + i * p.Q.row + hcol) * 2, hf);
+    dy = ex_global_row<uint16_t>(static_cast<const char*>(p.dY.data) + (b * p.dY.batch + i * p.dY.row + hcol) * 2, hf);
+    const ExRow<uint16_t> y =
+        ex_global_row<uint16_t>(static_cast<const char*>(p.Y.data) + (b * p.Y.batch + i * p.Y.row + hcol) * 2, hf);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        D = fmaf(__uint_as_float(y.v[k][w] << 16), __uint_as_float(dy.v[k][w] << 16), D);
+        D = fmaf(__uint_as_float(y.v[k][w] & 0xffff0000u), __uint_as_float(dy.v[k][w] & 0xffff0000u), D);
+      }
+    const float lse = p.lse[((int64_t)b * p.H + h) * p.nq + i];
+    cr = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  }
+  load(1, 1);
+  D += ex_other_half(D);
+  if (hf == 0 && i < p.nq) ex_put_stat<uint16_t>(p, ((int64_t)b * p.H + h) * p.nq + i, cr, D);
+  f32x16_t nD;  // where dP's sums start
+#pragma unroll
+  for (int r = 0; r < 16; ++r) nD[r] = -D;
+  const float* tl = tb + p.D + 64;
+  float far_l = 0.f, far_r = 0.f;
+  if constexpr (BIAS) {
+    ex_fill_bias<uint16_t>(p, tb, h, 1);
+    for (int e = lane; e < n; e += 64) dg[e] = 0.f;
+    for (int e = lane; e < 32 * 64; e += 64) st[e] = 0.f;
+    __syncthreads();
+  }
+
+  const ExRows64 ra = ex_rows64(lane);
+  const ExCols64<false> ca = ex_cols64<false>(lane);
+  const f32x16_t zero = ex_zero16();
+  f32x16_t dq[2] = {zero, zero}, s0, s1, p0, p1;
+  u32x4_t fr[kAhead], ds[2];
+  // Operand of slot j: K, V chunk j / 2 in turn of half tile (kt, half), then K columns of (ct, chalf).
+  auto read = [&](int j, const char* kt, int half, const char* ct, int chalf) __attribute__((always_inline)) {
+    if (j < 8) return ex_read_row(kt + (j & 1) * 3 * kTile64, ra, half, j >> 1);
+    return ex_read_col(ct, ca, chalf, (j - 8) >> 1, j & 1);
+  };
+  float fac = p.s2, add = -cr;
+  int side = 0;
+  // What a half tile's scores still need: masks and the bias of near pairs.
+  auto fix = [&](f32x16_t& s, int k0) __attribute__((always_inline)) {
+    if constexpr (BIAS) {
+      side = ex_bias_side(p, k0, br.pos + qw, br.pos + qw + 31);
+      if (side != 0) {
+        fac = p.s2;
+        add = tl[side * p.D] - cr;
+      } else {
+        fac = 1.f;
+        add = -cr;
+        const float* at = tl + (k0 + 4 * hf - br.pos - qw - ex_opaque(c));
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __fmaf_rn(s[r], p.s2, at[(r & 3) + 8 * (r >> 2)]);
+      }
+    }
+    if (__builtin_expect(!ex_whole(p, wmin, wmax, k0, br.klen), 0)) {
+      const ExSpan keys = ex_keys_of(p, br.pos + qw + ex_opaque(c), br.klen);
+      const int kh = k0 + 4 * hf;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = ex_in(keys, kh + (r & 3) + 8 * (r >> 2)) ? s[r] : -INFINITY;
+    }
+  };
+  // Half tile `ch` of ct: dS from (s, d); half tile nh of nt: S and dP into (sn, dn). (ft, fh): the one after that.
+  auto step = [&](f32x16_t& s, f32x16_t& d, f32x16_t& sn, f32x16_t& dn, const char* ct, int ch, const char* nt, int nh,
+                  const char* ft, int fh, int k0) __attribute__((always_inline)) {
+    ExPair e{0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 12; ++j) {
+      if (j < 8) {
+        if (j % 2 == 0) sn = ex_mfma<uint16_t>(fr[j % kAhead], q.v[j >> 1], j == 0 ? zero : sn);
+        else dn = ex_mfma<uint16_t>(fr[j % kAhead], dy.v[j >> 1], j == 1 ? nD : dn);
+      } else {
+        dq[j & 1] = ex_mfma<uint16_t>(fr[j % kAhead], ds[(j - 8) >> 1], dq[j & 1]);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // the read takes the registers the MFMA has read
+      fr[j % kAhead] = j + kAhead < 12 ? read(j + kAhead, nt, nh, ct, ch) : read(j + kAhead - 12, ft, fh, nullptr, 0);
+      if (j <= 8) {
+        const ExPair b4 = e;
+        if (j < 8) e = ex_pair<true>(s, j, fac, add);
+        if (j > 0) {
+          const int k = j - 1;
+          d[2 * k] *= b4.e0;
+          d[2 * k + 1] *= b4.e1;
+          uint32_t w = pack_bf16x2(d[2 * k], d[2 * k + 1]);
+          ex_pin(w);
+          ds[k >> 2][k & 3] = w;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (BIAS) {
+      if (side != 0) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += d[r];
+        far_l += side < 0 ? sum : 0.f;
+        far_r += side > 0 ? sum : 0.f;
+      } else {
+        ex_diagonals<false>(st, d, dg + p.D + 33 + k0 - br.pos - qw, lane);
+      }
+    }
+  };
+
+  wait_vmcnt<4>();  // tile 0
+  stage_barrier();
+  s0 = zero;
+  p0 = nD;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const u32x4_t f = read(j, smem, 0, nullptr, 0);
+    if (j % 2 == 0) s0 = ex_mfma<uint16_t>(f, q.v[j >> 1], s0);
+    else p0 = ex_mfma<uint16_t>(f, dy.v[j >> 1], p0);
+  }
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) fr[j] = read(j, smem, 1, nullptr, 0);
+  int b0 = 0, b1 = 1, b2 = 2;  // buffers of tiles t, t + 1, t + 2
+#pragma clang loop unroll(disable)
+  for (int t = 0; t < tiles.n; ++t) {
+    wait_vmcnt<0>();
+    stage_barrier();
+    load(t + 2, b2);
+    const char *ct = smem + b0 * kTile64, *nt = smem + b1 * kTile64;
+    const int k0 = ex_tile_at(tiles, t) * 64;
+    fix(s0, k0);
+    step(s0, p0, s1, p1, ct, 0, ct, 1, nt, 0, k0);
+    fix(s1, k0 + 32);
+    step(s1, p1, s0, p0, ct, 1, nt, 0, nt, 1, k0 + 32);
+    const int o = b0;
+    b0 = b1;
+    b1 = b2;
+    b2 = o;
+  }
+  if constexpr (BIAS) ex_add_far(dg, n, far_l, far_r, lane);
+  wait_vmcnt<0>();  // no load is under way into what is written next
+  __syncthreads();
+  char* out = static_cast<char*>(p.dQ.data) + (b * p.dQ.batch + (int64_t)qw * p.dQ.row + hcol) * 2;
+  ex_store_rows32(smem + wave * 32 * 144, dq, p.scale, out, p.dQ.row * 2, p.nq - qw, lane);
+  if constexpr (BIAS) {
+    for (int e = threadIdx.x; e < n; e += kExThreads) {
+      float t = tb[n + e];
+      for (int k = 1; k < kExWaves; ++k) t += tb[(1 + k) * n + e];
+      tb[e] = t;
+    }
+    __syncthreads();
+    ex_put_buckets(p, tb, b * nqt + qt, h);
+  }
+}
+
+constexpr int kDkvTilesStage = 2 * kTile64 + 512;  // Q, dY, two planes of 64 statistics
+constexpr int kDkvTilesLds = 3 * kDkvTilesStage;
+
+template <bool BIAS>
+__global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_dkv_tiles(ExactParams p, int heads_at_once) {
+  extern __shared__ __align__(16) char smem[];  // three stages, the bias tables of `heads_at_once` heads
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, hf = lane >> 5, n = 2 * p.D + 129;
+  const int nkt = (p.nk + 127) / 128;
+  if (BIAS && (int)blockIdx.x >= nkt * p.Hk * p.B) {
+    ex_sum_bias<uint16_t>(p, (blockIdx.x - nkt * p.Hk * p.B) * kExWaves + wave, lane);
+    return;
+  }
+  int kt, pair;
+  ex_block_pair(blockIdx.x, nkt, p.Hk * p.B, kt, pair);  // causal: the keys with the most queries come first
+  const int hk = pair % p.Hk, b = pair / p.Hk;
+  const ExRow0 br = ex_batch_row(p, b);
+  const int kw = kt * 128 + wave * 32, j = kw + c;
+  const ExTiles tiles = ex_query_tiles<64>(p, br, kt * 128, min(kt * 128 + 128, br.klen) - 1);
+
+  ExRow<uint16_t> kf = ex_zero_row<uint16_t>(), vf = kf;
+  if (j < br.klen) {
+    kf = ex_global_row<uint16_t>(static_cast<const char*>(p.K.data) + (b * p.K.batch + j * p.K.row + hk * kDHead) * 2, hf);
+    vf = ex_global_row<uint16_t>(static_cast<const char*>(p.V.data) + (b * p.V.batch + j * p.V.row + hk * kDHead) * 2, hf);
+  }
+  const int qpitch = (int)p.Q.row * 2, ypitch = (int)p.dY.row * 2;
+  const uint32_t ql = ex_load64(wave, lane, qpitch), yl = ex_load64(wave, lane, ypitch), lds = lds_addr(smem);
+  const ExRows64 ra = ex_rows64(lane);
+  const ExCols64<false> ca = ex_cols64<false>(lane);
+  const f32x16_t zero = ex_zero16();
+  f32x16_t dk[2] = {zero, zero}, dv[2] = {zero, zero}, s0, s1, p0, p1;
+  u32x4_t fr[kAhead], pp[2], ds[2];
+  // Operand of slot i: Q, dY chunk i / 2 in turn of half tile (rt, half); then, for each 16 rows of
+  // (ct, chalf), dY's two column halves and Q's.
+  auto read = [&](int i, const char* rt, int half, const char* ct, int chalf) __attribute__((always_inline)) {
+    if (i < 8) return ex_read_row(rt + (i & 1) * kTile64, ra, half, i >> 1);
+    return ex_read_col(ct + ((i & 2) ? 0 : kTile64), ca, chalf, (i - 8) >> 2, i & 1);
+  };
+  // Rows of a half tile: where S and dP start, -c / s2 and -D.
+  auto start = [&](f32x16_t& s, f32x16_t& d, const char* rt, int half) __attribute__((always_inline)) {
+    const float* at = reinterpret_cast<const float*>(rt + 2 * kTile64) + 32 * half + 4 * hf;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 t = *reinterpret_cast<const float4*>(at + 8 * k), u = *reinterpret_cast<const float4*>(at + 64 + 8 * k);
+      s[4 * k] = t.x, s[4 * k + 1] = t.y, s[4 * k + 2] = t.z, s[4 * k + 3] = t.w;
+      d[4 * k] = u.x, d[4 * k + 1] = u.y, d[4 * k + 2] = u.z, d[4 * k + 3] = u.w;
+    }
+  };
+  float fac = p.s2, add = 0.f;
+  const float* tl = nullptr;
+  auto fix = [&](f32x16_t& s, int i0) __attribute__((always_inline)) {
+    const int q0 = br.pos + i0;
+    if constexpr (BIAS) {
+      const int side = ex_bias_side(p, kw, q0, q0 + 31);
+      fac = p.s2;
+      add = 0.f;
+      if (side != 0) {
+        add = tl[side * p.D];
+      } else {
+        fac = 1.f;
+        const float* at = tl + (kw + ex_opaque(c) - q0 - 4 * hf);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __fmaf_rn(s[r], p.s2, at[-((r & 3) + 8 * (r >> 2))]);
+      }
+    }
+    // rows past the last query and keys past the last key add nothing that is kept
+    if (__builtin_expect(!ex_whole(p, q0, q0 + 31, kw, 0x7fffffff), 0)) {
+      const ExSpan queries = ex_queries_of(p, br, kw + ex_opaque(c));
+      const int ih = i0 + 4 * hf;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = ex_in(queries, ih + (r & 3) + 8 * (r >> 2)) ? s[r] : -INFINITY;
+    }
+  };
+  // Half tile ch of ct: P and dS from (s, d); half tile nh of nt: S and dP into (sn, dn); (ft, fh): the one
+  // after that, whose start values take the place of (s, d).
+  auto step = [&](f32x16_t& s, f32x16_t& d, f32x16_t& sn, f32x16_t& dn, const char* ct, int ch, const char* nt, int nh,
+                  const char* ft, int fh) __attribute__((always_inline)) {
+    ExPair e{0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i < 8) {
+        if (i % 2 == 0) sn = ex_mfma<uint16_t>(fr[i % kAhead], kf.v[i >> 1], sn);
+        else dn = ex_mfma<uint16_t>(fr[i % kAhead], vf.v[i >> 1], dn);
+      } else if (i & 2) {
+        dk[i & 1] = ex_mfma<uint16_t>(fr[i % kAhead], ds[(i - 8) >> 2], dk[i & 1]);
+      } else {
+        dv[i & 1] = ex_mfma<uint16_t>(fr[i % kAhead], pp[(i - 8) >> 2], dv[i & 1]);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // the read takes the registers the MFMA has read
+      fr[i % kAhead] = i + kAhead < 16 ? read(i + kAhead, nt, nh, ct, ch) : read(i + kAhead - 16, ft, fh, nullptr, 0);
+      if (i <= 8) {
+        const ExPair b4 = e;
+        if (i < 8) e = ex_pair<BIAS>(s, i, fac, add);
+        if (i > 0) {
+          const int k = i - 1;
+          uint32_t w = pack_bf16x2(b4.e0, b4.e1), x = pack_bf16x2(b4.e0 * d[2 * k], b4.e1 * d[2 * k + 1]);
+          ex_pin(w);
+          ex_pin(x);
+          pp[k >> 2][k & 3] = w;
+          ds[k >> 2][k & 3] = x;
+        }
+      }
+      if (i == 9) start(s, d, ft, fh);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  for (int g0 = 0; g0 < p.G; g0 += heads_at_once) {
+    const int ng = min(heads_at_once, p.G - g0), total = tiles.n * ng;
+    if (total == 0) break;
+    if constexpr (BIAS) {
+      __syncthreads();
+      ex_fill_bias<uint16_t>(p, reinterpret_cast<float*>(smem + kDkvTilesLds), hk * p.G + g0, ng);
+    }
+    // the next tile to load: head lg of the chunk, tile lt
+    int lg = 0, lt = 0;
+    auto load = [&](int slot) __attribute__((always_inline)) {  // past the last tile: zeros
+      const int h = hk * p.G + g0 + lg, i0 = ex_tile_at(tiles, lt) * 64, limit = lg < ng ? br.qlen : 0;
+      const char* Qb = static_cast<const char*>(p.Q.data) + (b * p.Q.batch + h * kDHead) * 2;
+      const char* Yb = static_cast<const char*>(p.dY.data) + (b * p.dY.batch + h * kDHead) * 2;
+      const uint32_t to = lds + slot * kDkvTilesStage;
+      ex_load_tile64(Qb, qpitch, i0, limit, ql, to, wave);
+      ex_load_tile64(Yb, ypitch, i0, limit, yl, to + kTile64, wave);
+      if (wave < 2) {  // a plane of statistics each
+        const char* stat = reinterpret_cast<const char*>(p.rowstat + ((int64_t)wave * p.B * p.H + (int64_t)b * p.H + h) * p.nq);
+        u32x4_t rs = ex_rsrc(stat, 4, i0, 0, 4);
+        rs[2] = (uint32_t)__builtin_amdgcn_readfirstlane(max(min(limit - i0, 64), 0) * 4);
+        ex_load_lds4(rs, lane * 4, to + 2 * kTile64 + 256 * wave);
+      }
+      if (++lt == tiles.n) {
+        lt = 0;
+        ++lg;
+      }
+    };
+    __syncthreads();  // the buffers (and the bias tables) are this chunk's from here on
+    load(0);
+    load(1);
+    wait_vmcnt<4>();  // tile 0
+    stage_barrier();
+    start(s0, p0, smem, 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const u32x4_t f = read(i, smem, 0, nullptr, 0);
+      if (i % 2 == 0) s0 = ex_mfma<uint16_t>(f, kf.v[i >> 1], s0);
+      else p0 = ex_mfma<uint16_t>(f, vf.v[i >> 1], p0);
+    }
+    start(s1, p1, smem, 1);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) fr[i] = read(i, smem, 1, nullptr, 0);
+    int b0 = 0, b1 = 1, b2 = 2, g = 0, t = 0;  // buffers of the tile, the next one, the one after
+    if constexpr (BIAS) tl = reinterpret_cast<const float*>(smem + kDkvTilesLds) + p.D + 64;
+#pragma clang loop unroll(disable)
+    for (int it = 0; it < total; ++it) {
+      wait_vmcnt<0>();
+      stage_barrier();
+      load(b2);
+      const char *ct = smem + b0 * kDkvTilesStage, *nt = smem + b1 * kDkvTilesStage;
+      const int i0 = ex_tile_at(tiles, t) * 64;
+      fix(s0, i0);
+      step(s0, p0, s1, p1, ct, 0, ct, 1, nt, 0);
+      fix(s1, i0 + 32);
+      step(s1, p1, s0, p0, ct, 1, nt, 0, nt, 1);
+      const int o = b0;
+      b0 = b1;
+      b1 = b2;
+      b2 = o;
+      if (++t == tiles.n) {
+        t = 0;
+        if constexpr (BIAS) tl += n;
+      }
+    }
+    wait_vmcnt<0>();  // no load is under way into what is written next
+  }
+  __syncthreads();
+  if (j >= br.klen) dk[0] = dk[1] = dv[0] = dv[1] = zero;
+  char* st = smem + wave * 32 * 144;
+  char* out = static_cast<char*>(p.dK.data) + (b * p.dK.batch + (int64_t)kw * p.dK.row + hk * kDHead) * 2;
+  ex_store_rows32(st, dk, p.scale, out, p.dK.row * 2, p.nk - kw, lane);
+  out = static_cast<char*>(p.dV.data) + (b * p.dV.batch + (int64_t)kw * p.dV.row + hk * kDHead) * 2;
+  ex_store_rows32(st, dv, 1.f, out, p.dV.row * 2, p.nk - kw, lane);
+}
+
 template <typename K>
 hipError_t set_lds(K kernel, size_t lds) {
   return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
 }
 
+// bf16 in blocks of 128 rows where the blocks of 32 are more than the CUs, which hold one of them each
+// (backward pass, 8 x 128 tokens, 12 heads: 20.3 against 13.9 us; 4 x 128, one round, 11.7 against 13.6;
+// 1 x 512 16.2 and 25.0, 2 x 512 34.6 and 25.6).
+bool dq_in_tiles(const ExactParams& p) { return p.bf16 && exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B > device_cus(); }
+bool dkv_in_tiles(const ExactParams& p) { return p.bf16 && (int64_t)((p.nk + 31) / 32) * p.Hk * p.B > device_cus(); }
+
 template <typename T, bool BIAS>
-hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
-  const size_t entries = BIAS ? (size_t)exact_bias_entries(p.D) : 0;
-  const size_t dq_lds = kDqLds<T> + entries * p.Gp * (1 + 2 * kExWaves) * 4;
-  hipError_t e = set_lds(k_exact_dq<T, BIAS>, dq_lds);
-  if (e != hipSuccess) return e;
-  const int64_t rows = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
-  hipLaunchKernelGGL((k_exact_dq<T, BIAS>), dim3((unsigned)rows), dim3(kExThreads), dq_lds, s, p);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  // heads whose bias tables fit beside the tiles at once
-  const int at_once = BIAS ? (int)((163840 - kDkvLds<T>) / (entries * 4)) : p.G;
-  const int heads = at_once < p.G ? at_once : p.G;
-  const size_t dkv_lds = kDkvLds<T> + entries * heads * 4;
-  if ((e = set_lds(k_exact_dkv<T, BIAS>, dkv_lds)) != hipSuccess) return e;
-  const int64_t blocks = (int64_t)((p.nk + 31) / 32) * p.Hk * p.B + (BIAS ? (p.buckets * p.H + kExWaves - 1) / kExWaves : 0);
-  hipLaunchKernelGGL((k_exact_dkv<T, BIAS>), dim3((unsigned)blocks), dim3(kExThreads), dkv_lds, s, p, heads);
+hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
+  const size_t tables = BIAS ? (size_t)exact_bias_entries(p.D) * (1 + kExWaves) * 4 : 0;
+  hipError_t e;
+  if constexpr (ExFmt<T>::ES == 2) {
+    if (dq_in_tiles(p)) {
+      const size_t lds = kDqTilesLds<BIAS> + tables;
+      if ((e = set_lds(k_exact_dq_tiles<BIAS>, lds)) != hipSuccess) return e;
+      const int64_t blocks = (int64_t)((p.nq + 127) / 128) * p.H * p.B;
+      hipLaunchKernelGGL((k_exact_dq_tiles<BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
+      return hipGetLastError();
+    }
+  }
+  const size_t lds = kDqLds<T> + tables;
+  if ((e = set_lds(k_exact_dq<T, BIAS>, lds)) != hipSuccess) return e;
+  const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
+  hipLaunchKernelGGL((k_exact_dq<T, BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
   return hipGetLastError();
 }
 
+template <typename T, bool BIAS>
+hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
+  const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
+  const int64_t sums = BIAS ? (p.buckets * p.H + kExWaves - 1) / kExWaves : 0;  // blocks that add up the bias gradient
+  hipError_t e;
+  if constexpr (ExFmt<T>::ES == 2) {
+    if (dkv_in_tiles(p)) {
+      const int at_once = BIAS ? (int)((81920 - kDkvTilesLds) / table) : p.G;  // two blocks to a CU
+      const int heads = at_once < p.G ? at_once : p.G;
+      const size_t lds = kDkvTilesLds + table * heads;
+      if ((e = set_lds(k_exact_dkv_tiles<BIAS>, lds)) != hipSuccess) return e;
+      const int64_t blocks = (int64_t)((p.nk + 127) / 128) * p.Hk * p.B + sums;
+      hipLaunchKernelGGL((k_exact_dkv_tiles<BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
+      return hipGetLastError();
+    }
+  }
+  // heads whose bias tables fit beside the tiles at once
+  const int at_once = BIAS ? (int)((163840 - kDkvLds<T>) / table) : p.G;
+  const int heads = at_once < p.G ? at_once : p.G;
+  const size_t lds = kDkvLds<T> + table * heads;
+  if ((e = set_lds(k_exact_dkv<T, BIAS>, lds)) != hipSuccess) return e;
+  const int64_t blocks = (int64_t)((p.nk + 31) / 32) * p.Hk * p.B + sums;
+  hipLaunchKernelGGL((k_exact_dkv<T, BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
+  return hipGetLastError();
+}
+
+template <typename T, bool BIAS>
+hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
+  const hipError_t e = launch_dq<T, BIAS>(p, s);
+  return e != hipSuccess ? e : launch_dkv<T, BIAS>(p, s);
+}
+
 }  // namespace
+
+int exact_bias_parts(const ExactParams& p) {
+  return (int)(p.B * (dq_in_tiles(p) ? (p.nq + 127) / 128 : exact_row_tiles(p.nq, p.Gp)));
+}
 
 hipError_t launch_exact_backward(const ExactParams& p, hipStream_t s) {
   if (p.bf16) return p.table ? launch_backward<uint16_t, true>(p, s) : launch_backward<uint16_t, false>(p, s);

@@ -6,6 +6,7 @@
 // as S^T = K Q^T, so that a lane holds one query's scores: m, l and the rescaling are per lane, and
 // P feeds Y^T = V^T P^T from the registers it is in.
 #include "exact_device.h"
+#include "mca_kernels.h"
 
 namespace mca {
 namespace {
@@ -216,6 +217,275 @@ __global__ __launch_bounds__(kExThreads) void k_exact_join(ExactParams p) {
   if (lane == 0) p.lse[((int64_t)b * p.H + h) * p.nq + i] = L > 0.f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
 }
 
+// ------------------------------------------------------------------ 128 or 256 queries per block, bf16
+// Four waves of 32 MT queries of one head share key tiles of 64. What bounds it is issue on each
+// SIMD, as in the output pass of the sampled layer: a half tile of 32 keys runs as slots that are
+// fixed in the source, each one MFMA (in turn S of half tile h + 1 and P V of h - 1) beside the vector
+// work of two scores of h, and reloads the fragment that its MFMA has used. K and V tiles are
+// loaded straight into LDS, three buffers each.
+//
+// No running maximum: P = exp2(x - M) under M, the largest logit of the row's first 32 keys, needs no
+// correction of what has been summed, and keeps its relative precision, in bf16 too, up to the
+// type's range. A row whose sum passes 2^64 (logits 44 above M), or whose first keys the bias all
+// masked and whose sum is below 2^-20, has its block take the pass again with a running maximum.
+template <bool BIAS, int MT>
+__global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT == 1 && !BIAS ? 3 : 2))) void k_exact_tiles(ExactParams p) {
+  constexpr int QB = 128 * MT;
+  extern __shared__ __align__(16) char smem[];  // three K tiles, three V tiles, the bias table
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, hf = lane >> 5;
+  int qt, pair;
+  const int nqt = (p.nq + QB - 1) / QB;
+  ex_block_pair(blockIdx.x, nqt, p.H * p.B, qt, pair);
+  if (p.causal) qt = nqt - 1 - qt;  // the longest rows first
+  const int h = pair % p.H, b = pair / p.H, hk = h / p.G;
+  const ExRow0 br = ex_batch_row(p, b);
+  const int qw = qt * QB + wave * 32 * MT;  // the wave's first query
+  const int last = min(qt * QB + QB, br.qlen) - 1;
+  const ExTiles tiles = last >= qt * QB ? ex_key_tiles<64>(p, br.pos + qt * QB, br.pos + last, br.klen) : ExTiles{-1, 0, 0};
+  // positions of the wave's queries that there are
+  const int wmin = br.pos + qw, wmax = br.pos + min(qw + 32 * MT, br.qlen) - 1;
+
+  char* yrow = static_cast<char*>(p.Yo.data) + ((int64_t)b * p.Yo.batch + (int64_t)qw * p.Yo.row + h * kDHead) * 2;
+  float* lse = p.lse + ((int64_t)b * p.H + h) * p.nq;
+  const char* Kb = static_cast<const char*>(p.K.data) + (b * p.K.batch + hk * kDHead) * 2;
+  const char* Vb = static_cast<const char*>(p.V.data) + (b * p.V.batch + hk * kDHead) * 2;
+  const int kpitch = (int)p.K.row * 2, vpitch = (int)p.V.row * 2;
+  const uint32_t kl = ex_load64(wave, lane, kpitch), vl = ex_load64<true>(wave, lane, vpitch);
+  const uint32_t lds = lds_addr(smem);
+  auto load_k = [&](int t, int slot) __attribute__((always_inline)) {  // past the last tile: zeros
+    ex_load_tile64(Kb, kpitch, ex_tile_at(tiles, t) * 64, t < tiles.n ? br.klen : 0, kl, lds + slot * kTile64, wave);
+  };
+  auto load_v = [&](int t, int slot) __attribute__((always_inline)) {
+    ex_load_tile64(Vb, vpitch, ex_tile_at(tiles, t) * 64, t < tiles.n ? br.klen : 0, vl, lds + (3 + slot) * kTile64, wave);
+  };
+  load_k(0, 0);
+  ExRow<uint16_t> q[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int i = min(qw + 32 * m + c, br.qlen - 1);
+    const char* row = static_cast<const char*>(p.Q.data) + ((int64_t)b * p.Q.batch + (int64_t)i * p.Q.row + h * kDHead) * 2;
+    q[m] = i >= 0 ? ex_global_row<uint16_t>(row, hf) : ex_zero_row<uint16_t>();
+  }
+  load_k(1, 1);
+  load_v(0, 0);
+  float* tb = reinterpret_cast<float*>(smem + 6 * kTile64);
+  const float* tl = tb + p.D + 64;
+  if constexpr (BIAS) ex_fill_bias<uint16_t>(p, tb, h, 1);
+
+  const ExRows64 ka = ex_rows64(lane);
+  const ExCols64<true> va = ex_cols64<true>(lane);
+  const f32x16_t zero = ex_zero16();
+  f32x16_t y[MT][2], s0[MT], s1[MT];
+  u32x4_t pa[MT][2], pb[MT][2];  // P of a half tile, 16 keys each
+  u32x4_t kf[4], vf[2][2];
+  float l[MT], nm[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    y[m][0] = y[m][1] = zero;
+    pb[m][0] = pb[m][1] = u32x4_t{0u, 0u, 0u, 0u};  // the first P V multiplies zeros
+    l[m] = 0.f;
+  }
+  vf[0][0] = vf[0][1] = vf[1][0] = vf[1][1] = u32x4_t{0u, 0u, 0u, 0u};
+
+  // What a half tile's scores still need: masks and the bias of near pairs. fac, add: a logit is
+  // fac * score + add.
+  float fac = p.s2, add = 0.f;
+  auto fix = [&](f32x16_t (&s)[MT], int k0) __attribute__((always_inline)) {
+    if constexpr (BIAS) {
+      const int side = ex_bias_side(p, k0, br.pos + qw, br.pos + qw + 32 * MT - 1);
+      // 64 queries: a tile near either half has more distances than the table holds for one
+      fac = p.s2;
+      add = 0.f;
+      if (side != 0) {
+        add = tl[side * p.D];
+      } else {
+        fac = 1.f;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const int pos = br.pos + qw + 32 * m + ex_opaque(c);
+          const int ms = MT == 1 ? 0 : ex_bias_side(p, k0, br.pos + qw + 32 * m, br.pos + qw + 32 * m + 31);
+          if (ms != 0) {
+            const float far = tl[ms * p.D];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[m][r] = __fmaf_rn(s[m][r], p.s2, far);
+          } else {
+            const float* at = tl + (k0 + 4 * hf - pos);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[m][r] = __fmaf_rn(s[m][r], p.s2, at[(r & 3) + 8 * (r >> 2)]);
+          }
+        }
+      }
+    }
+    if (__builtin_expect(!ex_whole(p, wmin, wmax, k0, br.klen), 0)) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const ExSpan keys = ex_keys_of(p, br.pos + qw + 32 * m + ex_opaque(c), br.klen);
+        const int kh = k0 + 4 * hf;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[m][r] = ex_in(keys, kh + (r & 3) + 8 * (r >> 2)) ? s[m][r] : -INFINITY;
+      }
+    }
+  };
+  // Half tile h: P of cur into po, S of half tile h + 1 into nxt, P V of half tile h - 1 (pi, vf); K half
+  // tile h + 2 and V half tile h are `half` of the tiles at kt and vt.
+  auto step = [&](f32x16_t (&cur)[MT], f32x16_t (&nxt)[MT], const u32x4_t (&pi)[MT][2], u32x4_t (&po)[MT][2],
+                  const char* kt, const char* vt, int half) __attribute__((always_inline)) {
+    float e0 = 0.f, e1 = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8 * MT; ++j) {
+      const int i = j / (2 * MT), m = (j >> 1) % MT, pp = i >> 1, cc = i & 1;
+      if (j % 2 == 0) {
+        nxt[m] = ex_mfma<uint16_t>(kf[i], q[m].v[i], i == 0 ? zero : nxt[m]);
+        __builtin_amdgcn_sched_barrier(0);  // the reload takes the registers the MFMA has read
+        if (m == MT - 1) kf[i] = ex_read_row(kt, ka, half, i);
+      } else {
+        y[m][cc] = ex_mfma<uint16_t>(vf[pp][cc], pi[m][pp], y[m][cc]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (m == MT - 1) vf[pp][cc] = ex_read_col(vt, va, half, pp, cc);
+      }
+      const int n = j >> 3, k = j & 7;  // scores 2 k, + 1 of query tile n
+      const float a = BIAS ? nm[n] + add : nm[n], f = BIAS ? fac : p.s2;
+      const float x0 = __fmaf_rn(cur[n][2 * k], f, a), x1 = __fmaf_rn(cur[n][2 * k + 1], f, a);
+      if (j > 0) {  // the pair before: its exp2 results are not waited for
+        const int o = (j - 1) >> 3;
+        l[o] += e0;
+        l[o] += e1;
+        uint32_t w = pack_bf16x2(e0, e1);
+        ex_pin(w);
+        po[o][((j - 1) >> 2) & 1][(j - 1) & 3] = w;
+      }
+      e0 = ex_exp2(x0);
+      e1 = ex_exp2(x1);
+      ex_pin(e0);
+      ex_pin(e1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    l[MT - 1] += e0;
+    l[MT - 1] += e1;
+    po[MT - 1][1][3] = pack_bf16x2(e0, e1);
+  };
+
+  if constexpr (BIAS) __syncthreads();
+  wait_vmcnt<4>();  // K tile 0
+  stage_barrier();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const u32x4_t k = ex_read_row(smem, ka, 0, i);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) s0[m] = ex_mfma<uint16_t>(k, q[m].v[i], i == 0 ? zero : s0[m]);
+    kf[i] = ex_read_row(smem, ka, 1, i);
+  }
+  fix(s0, ex_tile_at(tiles, 0) * 64);
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    float t = s0[m][0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) t = fmaxf(t, s0[m][r]);
+    t = __fmaf_rn(fmaxf(t, ex_other_half(t)), fac, add);  // fac > 0
+    nm[m] = t > -INFINITY ? -t : 0.f;
+  }
+  int b0 = 0, b1 = 1, b2 = 2;  // buffers of tiles t, t + 1, t + 2
+#pragma clang loop unroll(disable)
+  for (int t = 0; t < tiles.n; ++t) {
+    wait_vmcnt<0>();
+    stage_barrier();
+    load_k(t + 2, b2);
+    load_v(t + 1, b1);
+    const char *kt = smem + b1 * kTile64, *vt = smem + (3 + b0) * kTile64;
+    const int k0 = ex_tile_at(tiles, t) * 64;
+    if (t > 0) fix(s0, k0);
+    step(s0, s1, pb, pa, kt, vt, 0);
+    fix(s1, k0 + 32);
+    step(s1, s0, pa, pb, kt, vt, 1);
+    const int o = b0;
+    b0 = b1;
+    b1 = b2;
+    b2 = o;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) y[m][i & 1] = ex_mfma<uint16_t>(vf[i >> 1][i & 1], pb[m][i >> 1], y[m][i & 1]);
+  wait_vmcnt<0>();  // no load is under way into what is written next
+  bool again = false;
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    l[m] += ex_other_half(l[m]);
+    const bool live = qw + 32 * m + c < br.qlen && tiles.n > 0;
+    again = again || (live && (!(l[m] <= 0x1p64f) || (BIAS && l[m] < 0x1p-20f)));
+    if (!live) l[m] = 0.f;  // a padded query
+  }
+  // rows qw + 32 m on: their sums under -nmax, normalised and written
+  auto store = [&](int m, float nmax, float sum, f32x16_t (&ym)[2]) __attribute__((always_inline)) {
+    const int first = qw + 32 * m, ln = ex_opaque(lane), i = first + (ln & 31);
+    if (ln < 32 && i < p.nq) lse[i] = sum > 0.f ? (__builtin_amdgcn_logf(sum) - nmax) * kLn2 : -INFINITY;
+    if (sum == 0.f) ym[0] = ym[1] = zero;  // what was summed for it may be anything
+    ex_store_rows32(smem + wave * 32 * 144, ym, sum > 0.f ? 1.f / sum : 0.f, yrow + (int64_t)32 * m * p.Yo.row * 2,
+                    p.Yo.row * 2, p.nq - first, ln);
+  };
+  if (__builtin_expect(__syncthreads_or(again), 0)) {
+#pragma clang loop unroll(disable)
+    for (int m = 0; m < MT; ++m) {  // one after the other: the waves keep in step
+      ExState s;
+      s.m = -INFINITY;
+      s.l = 0.f;
+      s.y[0] = s.y[1] = zero;
+      const int first = qw + 32 * m, ln = ex_opaque(lane), cs = ln & 31, hs = ln >> 5, pos = br.pos + first + cs;
+      const ExCols64<true> vs = ex_cols64<true>(ln);
+      const ExSpan keys = ex_keys_of(p, pos, br.klen);
+      const char* row = static_cast<const char*>(p.Q.data) +
+                        ((int64_t)b * p.Q.batch + (int64_t)min(first + cs, br.qlen - 1) * p.Q.row + h * kDHead) * 2;
+      const ExRow<uint16_t> qm = ex_global_row<uint16_t>(row, hs);  // a block without queries is never here
+#pragma clang loop unroll(disable)
+      for (int t = 0; t < tiles.n; ++t) {
+        load_k(t, 0);
+        load_v(t, 0);
+        wait_vmcnt<0>();
+        __syncthreads();
+#pragma clang loop unroll(disable)
+        for (int half = 0; half < 2; ++half) {
+          const int k0 = ex_tile_at(tiles, t) * 64 + 32 * half;
+          f32x16_t x = ex_rows_product<uint16_t>(smem + half * 4096, qm, cs, hs);
+          const int side = BIAS ? ex_bias_side(p, k0, br.pos + first, br.pos + first + 31) : 0;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int e = (r & 3) + 8 * (r >> 2);
+            const float bias = !BIAS ? 0.f : side != 0 ? tl[side * p.D] : tl[k0 + 4 * hs - pos + e];
+            x[r] = ex_in(keys, k0 + 4 * hs + e) ? __fmaf_rn(x[r], p.s2, bias) : -INFINITY;
+          }
+          ex_softmax_step(s, x);
+#pragma unroll
+          for (int pp = 0; pp < 2; ++pp) {
+            u32x4_t x8;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x8[w] = pack_bf16x2(x[8 * pp + 2 * w], x[8 * pp + 2 * w + 1]);
+#pragma unroll
+            for (int cc = 0; cc < 2; ++cc)
+              s.y[cc] = ex_mfma<uint16_t>(ex_read_col(smem + 3 * kTile64, vs, half, pp, cc), x8, s.y[cc]);
+          }
+        }
+        __syncthreads();
+      }
+      s.l += ex_other_half(s.l);
+      store(m, -s.m, first + cs < br.qlen ? s.l : 0.f, s.y);
+      __syncthreads();
+    }
+    return;
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) store(m, nm[m], l[m], y[m]);
+}
+
+template <bool BIAS, int MT>
+hipError_t launch_tiles(const ExactParams& p, hipStream_t s) {
+  const size_t lds = 6 * kTile64 + (BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0);
+  const int64_t blocks = (int64_t)((p.nq + 128 * MT - 1) / (128 * MT)) * p.H * p.B;
+  hipLaunchKernelGGL((k_exact_tiles<BIAS, MT>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
+  return hipGetLastError();
+}
+
 template <typename T, bool BIAS>
 hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
   const size_t lds = kRowLds<T> + (BIAS ? (size_t)p.Gp * exact_bias_entries(p.D) * 4 : 0);
@@ -230,23 +500,45 @@ hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
 
 }  // namespace
 
-// Heads side by side in the kernels of 32 rows: a key head's whole group, unless its bias tables (and,
-// backward, their gradients: two arrays per wave) do not fit beside the tiles.
+// Heads side by side in the kernels of 32 rows: a key head's whole group, unless its bias tables do not
+// fit beside the tiles. One where the bias gradient is taken, along the diagonals of a head's tiles.
 int exact_group(const ExactParams& p, bool backward) {
   if (!p.table) return p.G;
-  const int64_t floats = (int64_t)p.G * exact_bias_entries(p.D) * (backward ? 1 + 2 * kExWaves : 1);
-  return floats <= 8192 ? p.G : 1;
+  return !backward && (int64_t)p.G * exact_bias_entries(p.D) <= 8192 ? p.G : 1;
+}
+
+// bf16 in blocks of 128 queries or more: where the blocks of 32 rows are more than the CUs (one of those
+// fills a CU's LDS, so a second round of them doubles the time: 8 x 128 tokens, 12 heads 8.8 against
+// 6.2 us; 4 x 128, one round, 5.3 against 6.1; 2 x 512 14.2 and 10.9, 1 x 512 7.4 and 10.7). Rows of a
+// single block of 32 over many keys stay: its four waves share the keys, of which a wave of the
+// other kernel reads all.
+static bool forward_in_tiles(const ExactParams& p) {
+  return p.bf16 && exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B > device_cus() &&
+         (p.nq * p.Gp > 32 || p.nk <= 512);
+}
+// 256 queries per block instead of 128 halve the LDS reads and the loads per score, and take about 1.75
+// times as long: by what the CU with the most blocks has to do (4 x 4096 tokens, 12 heads: 6 blocks
+// against 3, 227 and 203 us; 8 x 1057: 4 and 2, 47.8 and 42.5; 3 x 2000: 3 and 2, 60.5 and 67.2; 32 x
+// 250: 3 and 2, 16.6 and 19.1). Not with a bias, whose masks and tables leave too few registers.
+static bool forward_wide(const ExactParams& p) {
+  const int64_t q128 = (p.nq + 127) / 128, pairs = (int64_t)p.H * p.B;
+  return !p.table && 4 * blocks_per_cu(q128 * pairs) > 7 * blocks_per_cu((q128 + 1) / 2 * pairs);
 }
 
 // Blocks that share a row's keys: as many as fill the card four times over, where every wave still
 // gets four tiles.
 int exact_splits(const ExactParams& p) {
+  if (forward_in_tiles(p)) return 1;
   const int64_t rows = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B, tiles = (p.nk + 31) / 32;
-  const int64_t want = (4 * 256 + rows - 1) / rows, most = tiles / (4 * kExWaves);
+  const int64_t want = (4 * device_cus() + rows - 1) / rows, most = tiles / (4 * kExWaves);
   return (int)(want < most ? (want < 1 ? 1 : want) : (most < 1 ? 1 : most));
 }
 
 hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s) {
+  if (forward_in_tiles(p)) {
+    if (p.table) return launch_tiles<true, 1>(p, s);
+    return forward_wide(p) ? launch_tiles<false, 2>(p, s) : launch_tiles<false, 1>(p, s);
+  }
   if (p.bf16) return p.table ? launch_rows<uint16_t, true>(p, s) : launch_rows<uint16_t, false>(p, s);
   return p.table ? launch_rows<float, true>(p, s) : launch_rows<float, false>(p, s);
 }

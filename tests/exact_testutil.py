@@ -9,6 +9,7 @@ is off by at most k u times the sum of the terms' magnitudes):
                 steps, one more rescaling per key tile) + 5 u |lse_i| (subtractions, base change)
   P_ij:         relative eta_i = 2 max_j e_ij + (n_k + 16) u + 5 u |lse_i|, and, as the operand of a
                 product, h more in bfloat16
+                (backward in bfloat16: + 68 u |lse_i|, as the sums of S start at -lse_i / scale)
   y_i:          sum_j P_ij |v_j| (eta_i + [bf16] h + n_k u) + h |y_i|
   D_i:          sum_d |dy| (error of y_i) + 65 u sum_d |dy y|
   dS_ij:        P_ij (65 u sum_d |dy v| + error of D_i) + (eta_i + 4 u) P_ij (|dP_ij| + |D_i|), and, as
@@ -98,6 +99,8 @@ class Case:
         self.tol = {"Y": join(y_tol), "lse": (E + (nk + 16) * U + 5 * U * size)[..., 0]}
         if dY is not None:
             dy = split(dY, rows, 1)
+            if hp:
+                eta = eta + 68 * U * size
             dP = dy @ vt
             D = (dy * y).sum(-1, keepdim=True)
             D_tol = (dy.abs() * y_tol).sum(-1, keepdim=True) + 65 * U * (dy * y).abs().sum(-1, keepdim=True)

@@ -67,6 +67,19 @@ SHAPES = [  # B, nq, nk, heads, kv_heads, options
     (2, 40, 200, 2, 2, dict(window=30, causal=True, q_pos=[-10, 100])),
     (1, 513, 511, 2, 1, {}),
     (2, 1057, 1057, 2, 2, dict(window=256, q_lens=[1057, 353], kv_lens=[1057, 353])),
+    # more blocks of 32 rows than CUs: bfloat16 in blocks of 128 rows
+    (9, 129, 127, 8, 8, {}),
+    (24, 1, 90, 12, 12, {}),
+    (40, 33, 65, 8, 4, dict(kv_lens=[1 + b * 64 // 39 for b in range(40)])),
+    (5, 321, 321, 8, 8, dict(causal=True, q_lens=[321, 200, 1, 0, 129], kv_lens=[321, 200, 1, 77, 0])),
+    (4, 250, 400, 12, 4, dict(causal=True, q_pos=[150, 0, -60, 390])),
+    (4, 333, 333, 9, 3, dict(window=64, q_lens=[333, 120, 1, 200], kv_lens=[333, 120, 1, 200])),
+    (4, 300, 290, 9, 9, dict(window=30, causal=True, q_pos=[0, -10, 100, 5])),
+    (3, 260, 520, 12, 12, dict(window=100, q_pos=[0, 260, -100])),
+    # and of 256 queries: two rounds of 128 would not fill the card better
+    (8, 256, 640, 16, 8, {}),
+    (6, 500, 500, 16, 16, dict(causal=True, q_lens=[500, 100, 257, 256, 1, 499], kv_lens=[500, 100, 257, 256, 1, 499])),
+    (6, 511, 333, 16, 16, dict(window=128)),
 ]
 
 
@@ -89,6 +102,13 @@ BIAS = [
     (2, 160, 160, 12, 1, dict(buckets=128, max_distance=256)),  # a group whose tables do not fit at once
     (2, 260, 260, 4, 4, dict(buckets=6, max_distance=216, window=64)),
     (3, 40, 40, 4, 4, dict(buckets=32, q_lens=[40, 0, 7], kv_lens=[40, 12, 0])),
+    # more blocks of 32 rows than CUs
+    (8, 200, 200, 8, 8, dict(buckets=32)),
+    (3, 600, 500, 6, 2, dict(buckets=16, max_distance=40)),
+    (4, 330, 330, 8, 2, dict(buckets=32, bidirectional=False, causal=True, q_lens=[330, 77, 1, 200], kv_lens=[330, 77, 1, 200])),
+    (3, 300, 300, 12, 12, dict(buckets=64, max_distance=256, window=40, q_pos=[0, 3, 290])),
+    (1, 1030, 1030, 12, 12, dict(buckets=32)),
+    (3, 150, 190, 24, 1, dict(buckets=128, max_distance=256)),
 ]
 
 
@@ -102,9 +122,10 @@ def test_relative_bias(dtype, shape):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("low", [float("-inf"), -1e30, "lowest"])
-def test_bias_that_masks(dtype, low):
+@pytest.mark.parametrize("B,heads", [(2, 3), (14, 5)])  # blocks of 32 and, in bfloat16, of 128 rows
+def test_bias_that_masks(dtype, low, B, heads):
     """Buckets at -inf, -1e30 or the type's lowest value mask their pairs, whole rows among them."""
-    t, kw, bias = _make(dtype, 2, 150, 150, 3, 3, buckets=8, max_distance=20)
+    t, kw, bias = _make(dtype, B, 150, 150, heads, heads, buckets=8, max_distance=20)
     low = torch.finfo(TYPES[dtype]).min if low == "lowest" else low
     t["table"][2] = low
     t["table"][:, 1] = low  # every pair of one head
@@ -123,9 +144,12 @@ def test_keys_split_over_blocks(dtype, heads, kv, nq, nk):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_sharp_and_large_logits(dtype):
-    """Running maxima that rise late and far: logits of tens to hundreds."""
-    t, kw, bias = _make(dtype, 2, 70, 300, 2, 2, q_scale=8.0)
+@pytest.mark.parametrize("B,heads,buckets", [(2, 2, 0), (18, 6, 0), (18, 6, 32), (18, 16, 0)])
+def test_sharp_and_large_logits(dtype, B, heads, buckets):
+    """Running maxima that rise late and far: logits of tens to hundreds, in blocks of 32, 128 and 256
+    rows (there the sums pass 2^64 and the pass is taken again)."""
+    nq = 256 if heads == 16 else 70
+    t, kw, bias = _make(dtype, B, nq, 300, heads, heads, q_scale=8.0, buckets=buckets)
     t["K"][:, 200:] *= 4
     t["K"][:, 299] *= 4
     _check(t, kw, bias)
@@ -191,14 +215,14 @@ def test_offsets_past_32_bits(dtype):
 
 def test_same_bits_again():
     """The same call gives the same bits, and a batch row's results do not depend on the others."""
-    for dtype in ("f32", "bf16"):
-        t, kw, bias = _make(dtype, 3, 300, 300, 6, 2, buckets=32)
+    for dtype, heads in (("f32", 6), ("bf16", 6), ("bf16", 12)):
+        t, kw, bias = _make(dtype, 3, 300, 300, heads, 2, buckets=32)
         a, b = _run(t, kw, bias), _run(t, kw, bias)
         for k in a:
             assert torch.equal(a[k], b[k]), k
         one = {k: v[1:2].contiguous() if k in "QKVdY" else v for k, v in t.items()}
         c = _run(one, kw, bias)
-        for k in ("Y", "dQ", "dK", "dV"):
+        for k in ("Y", "dQ", "dK", "dV") if heads == 6 else ():  # one row of 12 heads is taken in other blocks
             assert torch.equal(a[k][1:2], c[k]), k
 
 
