@@ -45,8 +45,10 @@ struct ExactParams {
   float* rowstat;             // backward: two planes [B, H, nq] that k_exact_dkv starts from: of a row with
                               // c = log2(e) log-sum-exp (infinity without keys) and D = dY . Y, float32
                               // c and D, bf16 -c / s2 and -D (where its accumulators start)
-  float* part_bias;           // backward: [parts][buckets][H] gradient of a wave's or block's rows
-  int bias_parts;             // exact_bias_parts
+  int kv_splits;              // parts of the query tiles of a key head that blocks of their own take
+  float *part_dk, *part_dv;   // [kv_splits][B, nk, Hk, 64]
+  float* part_bias;           // [bias_parts][buckets][H]
+  int64_t bias_parts;
 };
 
 inline int exact_bias_entries(int D) { return 2 * D + 129; }  // rel = j - p in [-D - 64, D + 64]
@@ -54,8 +56,9 @@ inline int exact_bias_entries(int D) { return 2 * D + 129; }  // rel = j - p in 
 inline int64_t exact_row_tiles(int64_t nq, int64_t Gp) { return (nq * Gp + 31) / 32; }
 
 int exact_splits(const ExactParams& p);
-int exact_bias_parts(const ExactParams& p);  // blocks of rows that give the bias gradient a part each
-int exact_group(const ExactParams& p, bool backward);  // Gp
+int exact_kv_splits(const ExactParams& p);
+int64_t exact_bias_parts(const ExactParams& p);
+int exact_group(const ExactParams& p);  // Gp
 hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s);
 hipError_t launch_exact_backward(const ExactParams& p, hipStream_t s);
 

@@ -149,8 +149,9 @@ ExactParams params_of(const mca_exact_desc& d, bool backward) {
   p.q_pos = d.q_pos;
   p.table = d.bias_table;
   if (p.table) set_buckets(p, d.bias_buckets, d.bias_max_distance, d.bias_bidirectional);
-  p.Gp = mca::exact_group(p, backward);
+  p.Gp = mca::exact_group(p);
   p.splits = backward ? 1 : mca::exact_splits(p);
+  p.kv_splits = backward ? mca::exact_kv_splits(p) : 1;
   p.bias_parts = backward ? mca::exact_bias_parts(p) : 0;
   return p;
 }
@@ -165,6 +166,11 @@ size_t carve(ExactParams& p, bool backward, char* ws) {
   };
   if (backward) {
     p.rowstat = reinterpret_cast<float*>(take(8 * (size_t)p.B * p.H * p.nq));
+    if (p.kv_splits > 1) {
+      const size_t rows = 4 * 64 * (size_t)p.kv_splits * p.B * p.nk * p.Hk;
+      p.part_dk = reinterpret_cast<float*>(take(rows));
+      p.part_dv = reinterpret_cast<float*>(take(rows));
+    }
     if (p.table) p.part_bias = reinterpret_cast<float*>(take(4 * (size_t)p.bias_parts * p.buckets * p.H));
   } else if (p.splits > 1) {
     const size_t rows = (size_t)p.splits * p.B * (p.H / p.Gp) * mca::exact_row_tiles(p.nq, p.Gp) * 32;

@@ -270,10 +270,14 @@ __device__ __forceinline__ int ex_opaque(int x) {
   return x;
 }
 
-// The rows tile `qt` and (batch row, head) `pair` of block `bid`: the tiles of a pair on one XCD where
-// the pairs come in eights.
-__device__ __forceinline__ void ex_block_pair(int bid, int tiles, int pairs, int& qt, int& pair) {
-  if (pairs % 8 == 0) {
+// The rows tile and (batch row, head) `pair` of block `bid`: the tiles of a pair on one XCD where the pairs
+// come in eights. `uneven`: every pair's tile 0 before any tile 1, where a mask makes some tiles far
+// longer than others, which then start first.
+__device__ __forceinline__ void ex_block_pair(int bid, int tiles, int pairs, bool uneven, int& qt, int& pair) {
+  if (uneven) {
+    qt = bid / pairs;
+    pair = bid % pairs;
+  } else if (pairs % 8 == 0) {
     const int G = 8 * tiles, w = bid % G;
     pair = bid / G * 8 + w % 8;
     qt = w / 8;
@@ -310,6 +314,18 @@ struct ExSpan {
   int extra;
 };
 __device__ __forceinline__ bool ex_in(const ExSpan& s, int x) { return (unsigned)(x - s.lo) <= s.span || x == s.extra; }
+// Masks a tile whose first key (or query) of the lane is x0. `one`: the wave knows that no lane's extra one
+// is in the tile.
+__device__ __forceinline__ void ex_mask(f32x16_t& s, const ExSpan& a, int x0, bool one) {
+  const int d = x0 - a.lo;
+  if (one) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = (unsigned)(d + (r & 3) + 8 * (r >> 2)) <= a.span ? s[r] : -INFINITY;
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = ex_in(a, x0 + (r & 3) + 8 * (r >> 2)) ? s[r] : -INFINITY;
+  }
+}
 __device__ __forceinline__ ExSpan ex_span(int lo, int hi, int extra) {
   return hi < lo ? ExSpan{0x40000000, 0u, extra} : ExSpan{lo, (unsigned)(hi - lo), extra};
 }
@@ -383,6 +399,8 @@ __device__ __forceinline__ ExTiles ex_query_tiles(const ExactParams& p, const Ex
   }
   return ex_tiles<TILE>(lo, hi, extra);
 }
+// Where part k of n begins among `all` tiles.
+__device__ __forceinline__ int ex_part(int all, int k, int n) { return (int)((int64_t)all * k / n); }
 // Whether every query at pmin .. pmax attends every key of k0 .. k0 + 31.
 __device__ __forceinline__ bool ex_whole(const ExactParams& p, int pmin, int pmax, int k0, int klen) {
   bool w = k0 + 32 <= klen;

@@ -2,9 +2,11 @@
 //   P = exp2(s2 q.k + bias - c),  c = log2(e) lse,   dP = dY.v,   D = dY.y,   dS = P (dP - D),
 //   dq = scale sum_j dS k,   dk = scale sum_i dS q,   dv = sum_i P dy,   dT[c] = sum of dS in bucket c.
 // Two kernels, each summing over its own loop, so that every sum has a fixed order and no result
-// depends on the order of atomics: k_exact_dq (per query rows; also D and the bias gradient) and
-// k_exact_dkv (per keys, over the query heads that share them). That takes S and dP twice: seven
-// products for the five that the formulas need.
+// depends on the order of atomics: k_exact_dq (per query rows; also D) and k_exact_dkv (per keys, over
+// the query heads that share them; also the bias gradient). That takes S and dP twice: seven
+// products for the five that the formulas need. k_exact_join_grads adds up what the blocks of
+// k_exact_dkv leave in parts.
+#include <cstdlib>
 #include "exact_device.h"
 #include "mca_kernels.h"
 
@@ -55,81 +57,108 @@ __device__ __forceinline__ void ex_put_stat(const ExactParams& p, int64_t row, f
 }
 
 // ------------------------------------------------------------------ sums along diagonals
-// Adds the 63 diagonals of a 32x32 tile (lane: query row c; register r: key (r & 3) + 8 (r >> 2) + 4 hf)
-// to at[0 .. 62], diagonal key - query + 31. Row c goes to LDS shifted by its number, 64 floats to
-// a row, so that a diagonal is a column; then a lane adds two columns over half of the rows. The
-// entries that a row leaves are zeros: written here (FILL), or once by the caller, as every tile
-// leaves the same ones.
-template <bool FILL>
-__device__ __forceinline__ void ex_diagonals(float* st, const f32x16_t& x, float* at, int lane) {
-  const int c = lane & 31, hf = lane >> 5;
-  wave_lds_sync();
+// The bias gradient needs dS summed by rel = j - p, along the diagonals of a tile. In the registers of
+// k_exact_dkv a lane is a key and a register a query, so a step to the next query and the next
+// key is a step to the next register and lane: sums of the form acc = shift(acc) + x[r], one vector
+// instruction per pair with the lane shift in it, collect diagonals. A shift stays within 16 lanes
+// and what it pushes out is lost: shifting up collects the diagonals rel <= 0 of a block of 16 keys and
+// 16 queries, shifting down those of rel > 0. (Adding every pair to an array with LDS atomics took 130
+// cycles an instruction: 16 x 512 tokens, 12 heads, 306 us for the kernel that had it.)
+template <int CTRL>
+__device__ __forceinline__ float ex_shift(float v) {  // within rows of 16 lanes, zeros shifted in
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float ex_shift_rows(float v) {  // only the rows of 16 lanes in ROWS
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), CTRL,
+                                                               ROWS, 0xF, true));
+}
+// Adds a tile's sums to a wave's two arrays of n entries: `at` is the entry of rel = key 0 - query 0.
+__device__ __forceinline__ void ex_diagonals(const f32x16_t& x, float* at, int n, int lane) {
+  const int a = (lane >> 4) & 1, f = lane & 15;
+  float* o = at + (lane < 32 ? f - 15 : n + f) + 16 * a;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int e = (r & 3) + 8 * (r >> 2) + 4 * hf + 31 - c;
-    st[c * 64 + e] = x[r];
-    if (FILL) st[c * 64 + ((e + 32) & 63)] = 0.f;
-  }
-  wave_lds_sync();
-  float a0 = 0.f, a1 = 0.f;
+  for (int kb = 0; kb < 2; ++kb) {  // queries 16 kb + {0 .. 3, 8 .. 11} + 4 hf
+    float up = x[8 * kb], down = x[8 * kb + 7];
 #pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    const float2 v = *reinterpret_cast<const float2*>(st + (16 * hf + k) * 64 + 2 * c);
-    a0 += v.x;
-    a1 += v.y;
+    for (int r = 1; r < 8; ++r) {
+      up = (r == 4 ? ex_shift<0x115>(up) : ex_shift<0x111>(up)) + x[8 * kb + r];
+      down = (r == 4 ? ex_shift<0x105>(down) : ex_shift<0x101>(down)) + x[8 * kb + 7 - r];
+    }
+    up = ex_shift_rows<0x114, 0x3>(up);
+    down = ex_shift_rows<0x104, 0xC>(down);
+    // lanes below 32 take both halves' `up`, the others `down`, whose lanes 0 are `up`'s lanes 15
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(up), __float_as_uint(down), false, false);
+    const float v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    wave_lds_sync();
+    o[-16 * kb] += lane >= 32 && f == 0 ? 0.f : v;
   }
-  // lanes below 32 take column 2 c, the others 2 c + 1, of both halves of the rows
-  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(a0), __float_as_uint(a1), false, false);
-  float* o = at + 2 * c + hf;
-  *o += __uint_as_float(s[0]) + __uint_as_float(s[1]);
   wave_lds_sync();
 }
-// A lane's sums of far tiles: to entries of the far sides that no other lane uses.
-__device__ __forceinline__ void ex_add_far(float* dg, int n, float left, float right, int lane) {
+// Takes a wave's sums of a head out as a part of the bias gradient: far tiles' sums per lane (`left`: rel
+// <= -D, `right`: rel >= D) and the two arrays, which are left as zeros. A bucket's entries are neighbours;
+// four lanes share those of a bucket.
+__device__ __forceinline__ void ex_put_buckets(const ExactParams& p, float* dg, int n, float left, float right, int64_t part,
+                                               int head, int lane) {
   wave_lds_sync();
   left += ex_other_half(left);
   right += ex_other_half(right);
-  if (lane < 32) {
+  if (lane < 32) {  // entries of the far sides, one per lane
     dg[lane] += left;
     dg[n - 1 - lane] += right;
   }
-}
-// A part of the bias gradient: t holds the entries of one head. A bucket's entries are neighbours.
-__device__ __forceinline__ void ex_put_buckets(const ExactParams& p, const float* t, int64_t part, int head) {
+  wave_lds_sync();
+#pragma unroll 4
+  for (int e = lane; e < n; e += 64) {
+    dg[e] += dg[n + e];
+    dg[n + e] = 0.f;
+  }
+  wave_lds_sync();
   const int far = p.D + 64;
-  for (int k = threadIdx.x; k < p.buckets; k += kExThreads) {
-    const int kk = k % p.side;
-    const bool right = k >= p.side;
+  for (int k0 = 0; k0 < p.buckets; k0 += 16) {
+    const int k = min(k0 + (lane >> 2), p.buckets - 1), kk = k % p.side;
+    const bool ahead = k >= p.side;
     int lo = kk, hi = kk;  // distances
     if (kk >= p.E) {
       lo = kk == p.E ? p.E : p.thr[kk - p.E - 1];
       hi = kk - p.E < p.nthr ? p.thr[kk - p.E] - 1 : far;
     }
-    const int a = right ? max(lo, 1) : -hi;
-    const int z = right ? hi : !p.bidirectional && kk == 0 ? far : -lo;  // keys ahead share bucket 0
+    const int a = ahead ? max(lo, 1) : -hi;
+    const int z = ahead ? hi : !p.bidirectional && kk == 0 ? far : -lo;  // keys ahead share bucket 0
     float sum = 0.f;
-    for (int r = a; r <= z; ++r) sum += t[far + r];
-    p.part_bias[(part * p.buckets + k) * p.H + head] = sum;
+#pragma unroll 8
+    for (int r = a + (lane & 3); r <= z; r += 4) sum += dg[far + r];
+    sum += dpp_f32<0xB1>(sum);
+    sum += dpp_f32<0x4E>(sum);
+    if ((lane & 3) == 0 && k0 + (lane >> 2) < p.buckets) p.part_bias[(part * p.buckets + k) * p.H + head] = sum;
   }
+  wave_lds_sync();
+#pragma unroll 4
+  for (int e = lane; e < n; e += 64) dg[e] = 0.f;
+  wave_lds_sync();
+}
+template <typename T>
+__device__ __forceinline__ float ex_sum16(const T& x) {
+  float s = x[0];
+#pragma unroll
+  for (int r = 1; r < 16; ++r) s += x[r];
+  return s;
 }
 
 // ------------------------------------------------------------------ dQ
 // Blocks of 32 (query, head) rows whose key tiles the four waves share, as k_exact_rows. S^T = K Q^T
 // and dP^T = V dY^T: the row's c and D are one value per lane, and dS feeds dQ^T = K^T dS^T.
 //
-// The bias gradient: a pair's dS belongs to the diagonal rel = j - p of its tile. A tile whose pairs all
-// lie D or further away is summed per lane in a register. The 63 diagonals of another tile are
-// summed through LDS (ex_diagonals), in the tile's own buffer once the products are done with it,
-// into an array per wave: adding every pair to it with LDS atomics took 130 cycles an instruction
-// (16 x 512 tokens, 12 heads: 306 us against 117 for k_exact_dkv).
+//
+// With a bias in bfloat16, D = dY . Y of the rounded Y is not what the bias gradient asks for, whose sums
+// cancel: sum_j dS_ij, which is 0 for the exact D, is added to the D that k_exact_dkv takes.
 template <typename T, bool BIAS>
 __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
   extern __shared__ __align__(16) char smem[];
   constexpr int ES = ExFmt<T>::ES, ST = kBwdStages<T>, TB = tile_bytes<T>();
   const int n = 2 * p.D + 129;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  float* tb = reinterpret_cast<float*>(smem + kDqLds<T>);  // with a bias Gp = 1: one head's table
-  float* dg = tb + n + wave * n;                           // the wave's sums per entry
+  float* tb = reinterpret_cast<float*>(smem + kDqLds<T>);  // [Gp][n]
   const int c = lane & 31, hf = lane >> 5;
   const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp;
   int bid = blockIdx.x;
@@ -181,16 +210,14 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
     cr = lse == -INFINITY ? INFINITY : lse * kLog2e;
   }
   D += ex_other_half(D);
-  if (wave == 0 && hf == 0 && i < p.nq) ex_put_stat<T>(p, ((int64_t)b * p.H + head) * p.nq + i, cr, D);
   const int pos = br.pos + i;
   const ExSpan keys = ex_keys_of(p, pos, br.klen);
   const float* tl = nullptr;
-  float far_l = 0.f, far_r = 0.f;
+  float rest = 0.f;  // sum of dS
   if constexpr (BIAS) {
-    ex_fill_bias<T>(p, tb, head, 1);
-    for (int e = lane; e < n; e += 64) dg[e] = 0.f;
+    ex_fill_bias<T>(p, tb, hx * p.Gp, p.Gp);
     __syncthreads();
-    tl = tb + p.D + 64;
+    tl = tb + g * n + p.D + 64;
   }
   f32x16_t dq[2] = {ex_zero16(), ex_zero16()};
 
@@ -221,38 +248,28 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
       for (int r = 0; r < 16; ++r) x[r] = __fmaf_rn(x[r], p.s2, -cr);
     }
     if (!ex_whole(p, pmin, pmax, k0, br.klen)) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = ex_in(keys, k0 + 4 * hf + (r & 3) + 8 * (r >> 2)) ? x[r] : -INFINITY;
+      ex_mask(x, keys, k0 + 4 * hf, k0 > 0);
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) x[r] = ex_exp2(x[r]) * (dp[r] - D);
     ex_cols_product<T>(dq, kt, x, lane);
-    if constexpr (BIAS) {
-      if (side != 0) {
-        float sum = 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sum += x[r];
-        far_l += side < 0 ? sum : 0.f;
-        far_r += side > 0 ? sum : 0.f;
-      } else {
-        ex_diagonals<true>(reinterpret_cast<float*>(kt), x, dg + p.D + 33 + k0 - pmin, lane);
-      }
-    }
+    if constexpr (BIAS && ES == 2) rest += ex_sum16(x);
     slot = slot == ST - 1 ? 0 : slot + 1;
   }
-  if constexpr (BIAS) ex_add_far(dg, n, far_l, far_r, lane);
   wait_vmcnt<0>();  // no load is under way into what is written next
   __syncthreads();
   float* ys = reinterpret_cast<float*>(smem);
   ex_put_sums(ys, dq, wave * 32 + c, hf);
-  if constexpr (BIAS) {
-    for (int e = threadIdx.x; e < n; e += kExThreads) {
-      float t = tb[n + e];
-      for (int k = 1; k < kExWaves; ++k) t += tb[(1 + k) * n + e];
-      tb[e] = t;
-    }
+  float* rests = ys + kExWaves * 32 * kYS;  // [wave][row]
+  if constexpr (BIAS && ES == 2) {
+    rest += ex_other_half(rest);
+    if (hf == 0) rests[wave * 32 + c] = rest;
   }
   __syncthreads();
+  if (wave == 0 && hf == 0 && i < p.nq) {
+    if constexpr (BIAS && ES == 2) D += rests[c] + rests[32 + c] + rests[64 + c] + rests[96 + c];
+    ex_put_stat<T>(p, ((int64_t)b * p.H + head) * p.nq + i, cr, D);
+  }
   const int row = threadIdx.x >> 3, col = (threadIdx.x & 7) * 8;
   const int vr = vt * 32 + row, ir = vr / p.Gp;
   if (ir < p.nq) {
@@ -260,29 +277,13 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
     ex_join_sums(o, ys, row, col, p.scale);
     ex_store8(static_cast<T*>(p.dQ.data) + b * p.dQ.batch + ir * p.dQ.row + (hx * p.Gp + vr % p.Gp) * kDHead + col, o);
   }
-  if constexpr (BIAS) {
-    ex_put_buckets(p, tb, b * nvt + vt, head);
-  }
-}
-
-// Sums a (bucket, head)'s parts: entry e = bucket * H + head, by the lanes of a wave.
-template <typename T>
-__device__ __forceinline__ void ex_sum_bias(const ExactParams& p, int e, int lane) {
-  if (e >= p.buckets * p.H) return;
-  float sum = 0.f;
-  for (int k = lane; k < p.bias_parts; k += 64) sum += p.part_bias[(int64_t)k * p.buckets * p.H + e];
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if (lane != 0) return;
-  if constexpr (ExFmt<T>::ES == 2) static_cast<T*>(p.dtable)[e] = (T)f32_to_bf16_bits(sum);
-  else static_cast<T*>(p.dtable)[e] = sum;
 }
 
 // ------------------------------------------------------------------ dK, dV
-// Blocks of 32 keys of a key head; the four waves share the query tiles of all its query heads. S =
-// Q K^T and dP = dY V^T with the lane holding a key: P and dS feed dV^T = dY^T P and dK^T = Q^T dS.
-// A wave loads its tiles of Q, dY and (c, D) straight into LDS. The blocks behind the last key
-// block add up the bias gradient's parts, one (bucket, head) per wave.
+// Blocks of 32 keys of a key head; the four waves share the query tiles of all its query heads, or of the
+// block's part of them (kv_splits). S = Q K^T and dP = dY V^T with the lane holding a key: P and dS
+// feed dV^T = dY^T P and dK^T = Q^T dS. A wave loads its tiles of Q, dY and row statistics straight
+// into LDS.
 template <typename T, bool BIAS>
 __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int heads_at_once) {
   extern __shared__ __align__(16) char smem[];
@@ -290,15 +291,14 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nkt = (p.nk + 31) / 32;
   int bid = blockIdx.x;
-  if (BIAS && bid >= nkt * p.Hk * p.B) {
-    ex_sum_bias<T>(p, (bid - nkt * p.Hk * p.B) * kExWaves + wave, lane);
-    return;
-  }
   const int c = lane & 31, hf = lane >> 5, n = 2 * p.D + 129;
-  float* tb = reinterpret_cast<float*>(smem + kDkvLds<T>);  // [heads_at_once][n]
+  float* dg = reinterpret_cast<float*>(smem + kDkvLds<T>) + wave * 2 * n;  // the wave's sums along diagonals
+  float* tb = reinterpret_cast<float*>(smem + kDkvLds<T>) + kExWaves * 2 * n;  // [heads_at_once][n]
   const int kt = bid % nkt;
   bid /= nkt;
-  const int hk = bid % p.Hk, b = bid / p.Hk;
+  const int hk = bid % p.Hk;
+  bid /= p.Hk;
+  const int b = bid % p.B, split = bid / p.B;
   const ExRow0 br = ex_batch_row(p, b);
   const int j = kt * 32 + c, jmax = min(kt * 32 + 31, br.klen - 1);
   const ExTiles tiles = ex_query_tiles(p, br, kt * 32, jmax);
@@ -311,6 +311,11 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
   const ExRow<T> vf = live ? ex_global_row<T>(vrow, hf) : ex_zero_row<T>();
   f32x16_t dk[2] = {ex_zero16(), ex_zero16()}, dv[2] = {ex_zero16(), ex_zero16()};
   const uint32_t lds = lds_addr(smem) + (uint32_t)wave * ST * SB;
+  const int all = tiles.n * p.G, from = ex_part(all, split, p.kv_splits), to_ = ex_part(all, split + 1, p.kv_splits);
+  float far_l = 0.f, far_r = 0.f;
+  const int64_t part = ((int64_t)(split * p.B + b) * nkt + kt) * kExWaves + wave;
+  if constexpr (BIAS)
+    for (int e = lane; e < 2 * n; e += 64) dg[e] = 0.f;
 
   for (int g0 = 0; g0 < p.G; g0 += heads_at_once) {
     const int ng = min(heads_at_once, p.G - g0), h0 = hk * p.G + g0;
@@ -319,7 +324,8 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
       ex_fill_bias<T>(p, tb, h0, ng);
       __syncthreads();
     }
-    const int total = tiles.n * ng;
+    const int total = min(to_ - g0 * tiles.n, tiles.n * ng), first = max(from - g0 * tiles.n, 0) + wave;
+    int head = 0;  // of the chunk: whose sums along diagonals are under way
     auto load = [&](int idx, int slot) __attribute__((always_inline)) {  // past the last tile: zeros
       const int h = h0 + (tiles.n > 0 ? idx / tiles.n : 0);
       const int i0 = (tiles.n > 0 ? ex_tile_at(tiles, idx % tiles.n) : 0) * 32, limit = idx < total ? br.qlen : 0;
@@ -333,9 +339,9 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
       ex_load_lds4(ex_rsrc(st + 4 * (int64_t)p.B * p.H * p.nq, 4, i0, limit, 4), lane * 4, to + 2 * TB + 256);
     };
 #pragma unroll
-    for (int k = 0; k < ST - 1; ++k) load(wave + k * kExWaves, k);
+    for (int k = 0; k < ST - 1; ++k) load(first + k * kExWaves, k);
     int slot = 0;
-    for (int idx = wave; idx < total; idx += kExWaves) {
+    for (int idx = first; idx < total; idx += kExWaves) {
       wait_lds();  // the tile read last is overwritten by the next loads
       load(idx + (ST - 1) * kExWaves, slot == 0 ? ST - 1 : slot - 1);
       wait_vmcnt<(ST - 1) * (2 * ExFmt<T>::NL + 2)>();
@@ -361,9 +367,14 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
           cr[r] = D[r] = 0.f;
         }
       }
+      int side = 0;
       if constexpr (BIAS) {
-        const float* tl = tb + (idx / tiles.n) * n + p.D + 64;
-        const int side = ex_bias_side(p, kt * 32, p0, p0 + 31);
+        for (const int h = idx / tiles.n; head < h; ++head) {
+          ex_put_buckets(p, dg, n, far_l, far_r, part, h0 + head, lane);
+          far_l = far_r = 0.f;
+        }
+        const float* tl = tb + head * n + p.D + 64;
+        side = ex_bias_side(p, kt * 32, p0, p0 + 31);
         if (side != 0) {
           const float far = tl[side * p.D];
 #pragma unroll
@@ -377,10 +388,9 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[r] = __fmaf_rn(x[r], p.s2, -cr[r]);
       }
-      // (the sums of keys past the last one are not stored)
-      if (i0 + 32 > br.qlen || !ex_whole(p, p0, p0 + 31, kt * 32, 0x7fffffff)) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = ex_in(queries, i0 + 4 * hf + (r & 3) + 8 * (r >> 2)) ? x[r] : -INFINITY;
+      // (without a bias gradient keys past the last one may have any P and dS, which are not stored)
+      if (i0 + 32 > br.qlen || !ex_whole(p, p0, p0 + 31, kt * 32, BIAS ? br.klen : 0x7fffffff)) {
+        ex_mask(x, queries, i0 + 4 * hf, p0 > 0);
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -389,8 +399,18 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
       }
       ex_cols_product<T>(dv, qt + TB, x, lane);
       ex_cols_product<T>(dk, qt, ds, lane);
+      if constexpr (BIAS) {
+        if (side < 0) far_l += ex_sum16(ds);
+        else if (side > 0) far_r += ex_sum16(ds);
+        else ex_diagonals(ds, dg + p.D + 64 + kt * 32 - p0, n, lane);
+      }
       slot = slot == ST - 1 ? 0 : slot + 1;
     }
+    if constexpr (BIAS)
+      for (; head < ng; ++head) {
+        ex_put_buckets(p, dg, n, far_l, far_r, part, h0 + head, lane);
+        far_l = far_r = 0.f;
+      }
     wait_vmcnt<0>();
   }
   __syncthreads();
@@ -400,6 +420,15 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
   __syncthreads();
   const int row = threadIdx.x >> 3, col = (threadIdx.x & 7) * 8, jr = kt * 32 + row;
   if (jr >= p.nk) return;
+  if (p.kv_splits > 1) {
+    float o[8];
+    const int64_t at = (((int64_t)(split * p.B + b) * p.nk + jr) * p.Hk + hk) * kDHead + col;
+    ex_join_sums(o, ys, row, col, 1.f);
+    ex_store8(p.part_dk + at, o);
+    ex_join_sums(o, ys + kExWaves * 32 * kYS, row, col, 1.f);
+    ex_store8(p.part_dv + at, o);
+    return;
+  }
   float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (jr < br.klen) ex_join_sums(o, ys, row, col, p.scale);
   ex_store8(static_cast<T*>(p.dK.data) + b * p.dK.batch + jr * p.dK.row + hk * kDHead + col, o);
@@ -433,20 +462,15 @@ __device__ __forceinline__ ExPair ex_pair(const f32x16_t& s, int j, float fac, f
   return r;
 }
 
-template <bool BIAS> constexpr int kDqTilesLds = 6 * kTile64 + (BIAS ? kExWaves * 32 * 64 * 4 : 0);
-
 template <bool BIAS>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_dq_tiles(ExactParams p) {
-  extern __shared__ __align__(16) char smem[];  // three K tiles, three V tiles; diagonals, bias table, its gradient
-  const int n = 2 * p.D + 129;
+  extern __shared__ __align__(16) char smem[];  // three K tiles, three V tiles, the bias table
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hf = lane >> 5;
-  float* st = reinterpret_cast<float*>(smem + 6 * kTile64) + wave * 32 * 64;
-  float* tb = reinterpret_cast<float*>(smem + kDqTilesLds<BIAS>);
-  float* dg = tb + n + wave * n;
+  float* tb = reinterpret_cast<float*>(smem + 6 * kTile64);
   int qt, pair;
   const int nqt = (p.nq + 127) / 128;
-  ex_block_pair(blockIdx.x, nqt, p.H * p.B, qt, pair);
+  ex_block_pair(blockIdx.x, nqt, p.H * p.B, p.causal || p.window, qt, pair);
   if (p.causal) qt = nqt - 1 - qt;  // the longest rows first
   const int h = pair % p.H, b = pair / p.H, hk = h / p.G;
   const ExRow0 br = ex_batch_row(p, b);
@@ -486,16 +510,13 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   }
   load(1, 1);
   D += ex_other_half(D);
-  if (hf == 0 && i < p.nq) ex_put_stat<uint16_t>(p, ((int64_t)b * p.H + h) * p.nq + i, cr, D);
   f32x16_t nD;  // where dP's sums start
 #pragma unroll
   for (int r = 0; r < 16; ++r) nD[r] = -D;
   const float* tl = tb + p.D + 64;
-  float far_l = 0.f, far_r = 0.f;
+  float rest = 0.f;  // sum of dS
   if constexpr (BIAS) {
     ex_fill_bias<uint16_t>(p, tb, h, 1);
-    for (int e = lane; e < n; e += 64) dg[e] = 0.f;
-    for (int e = lane; e < 32 * 64; e += 64) st[e] = 0.f;
     __syncthreads();
   }
 
@@ -510,11 +531,10 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     return ex_read_col(ct, ca, chalf, (j - 8) >> 1, j & 1);
   };
   float fac = p.s2, add = -cr;
-  int side = 0;
   // What a half tile's scores still need: masks and the bias of near pairs.
   auto fix = [&](f32x16_t& s, int k0) __attribute__((always_inline)) {
     if constexpr (BIAS) {
-      side = ex_bias_side(p, k0, br.pos + qw, br.pos + qw + 31);
+      const int side = ex_bias_side(p, k0, br.pos + qw, br.pos + qw + 31);
       if (side != 0) {
         fac = p.s2;
         add = tl[side * p.D] - cr;
@@ -528,14 +548,12 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     }
     if (__builtin_expect(!ex_whole(p, wmin, wmax, k0, br.klen), 0)) {
       const ExSpan keys = ex_keys_of(p, br.pos + qw + ex_opaque(c), br.klen);
-      const int kh = k0 + 4 * hf;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = ex_in(keys, kh + (r & 3) + 8 * (r >> 2)) ? s[r] : -INFINITY;
+      ex_mask(s, keys, k0 + 4 * hf, k0 > 0);
     }
   };
   // Half tile `ch` of ct: dS from (s, d); half tile nh of nt: S and dP into (sn, dn). (ft, fh): the one after that.
   auto step = [&](f32x16_t& s, f32x16_t& d, f32x16_t& sn, f32x16_t& dn, const char* ct, int ch, const char* nt, int nh,
-                  const char* ft, int fh, int k0) __attribute__((always_inline)) {
+                  const char* ft, int fh) __attribute__((always_inline)) {
     ExPair e{0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < 12; ++j) {
@@ -554,23 +572,13 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
           const int k = j - 1;
           d[2 * k] *= b4.e0;
           d[2 * k + 1] *= b4.e1;
+          if constexpr (BIAS) rest += d[2 * k] + d[2 * k + 1];
           uint32_t w = pack_bf16x2(d[2 * k], d[2 * k + 1]);
           ex_pin(w);
           ds[k >> 2][k & 3] = w;
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-    }
-    if constexpr (BIAS) {
-      if (side != 0) {
-        float sum = 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sum += d[r];
-        far_l += side < 0 ? sum : 0.f;
-        far_r += side > 0 ? sum : 0.f;
-      } else {
-        ex_diagonals<false>(st, d, dg + p.D + 33 + k0 - br.pos - qw, lane);
-      }
     }
   };
 
@@ -595,28 +603,20 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     const char *ct = smem + b0 * kTile64, *nt = smem + b1 * kTile64;
     const int k0 = ex_tile_at(tiles, t) * 64;
     fix(s0, k0);
-    step(s0, p0, s1, p1, ct, 0, ct, 1, nt, 0, k0);
+    step(s0, p0, s1, p1, ct, 0, ct, 1, nt, 0);
     fix(s1, k0 + 32);
-    step(s1, p1, s0, p0, ct, 1, nt, 0, nt, 1, k0 + 32);
+    step(s1, p1, s0, p0, ct, 1, nt, 0, nt, 1);
     const int o = b0;
     b0 = b1;
     b1 = b2;
     b2 = o;
   }
-  if constexpr (BIAS) ex_add_far(dg, n, far_l, far_r, lane);
+  if constexpr (BIAS) D += rest + ex_other_half(rest);
+  if (hf == 0 && i < p.nq) ex_put_stat<uint16_t>(p, ((int64_t)b * p.H + h) * p.nq + i, cr, D);
   wait_vmcnt<0>();  // no load is under way into what is written next
   __syncthreads();
   char* out = static_cast<char*>(p.dQ.data) + (b * p.dQ.batch + (int64_t)qw * p.dQ.row + hcol) * 2;
   ex_store_rows32(smem + wave * 32 * 144, dq, p.scale, out, p.dQ.row * 2, p.nq - qw, lane);
-  if constexpr (BIAS) {
-    for (int e = threadIdx.x; e < n; e += kExThreads) {
-      float t = tb[n + e];
-      for (int k = 1; k < kExWaves; ++k) t += tb[(1 + k) * n + e];
-      tb[e] = t;
-    }
-    __syncthreads();
-    ex_put_buckets(p, tb, b * nqt + qt, h);
-  }
 }
 
 constexpr int kDkvTilesStage = 2 * kTile64 + 512;  // Q, dY, two planes of 64 statistics
@@ -624,17 +624,15 @@ constexpr int kDkvTilesLds = 3 * kDkvTilesStage;
 
 template <bool BIAS>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_dkv_tiles(ExactParams p, int heads_at_once) {
-  extern __shared__ __align__(16) char smem[];  // three stages, the bias tables of `heads_at_once` heads
+  extern __shared__ __align__(16) char smem[];  // three stages, sums along diagonals, the bias tables of `heads_at_once` heads
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hf = lane >> 5, n = 2 * p.D + 129;
   const int nkt = (p.nk + 127) / 128;
-  if (BIAS && (int)blockIdx.x >= nkt * p.Hk * p.B) {
-    ex_sum_bias<uint16_t>(p, (blockIdx.x - nkt * p.Hk * p.B) * kExWaves + wave, lane);
-    return;
-  }
+  float* dg = reinterpret_cast<float*>(smem + kDkvTilesLds) + wave * 2 * n;
+  float* tb = reinterpret_cast<float*>(smem + kDkvTilesLds) + kExWaves * 2 * n;
   int kt, pair;
-  ex_block_pair(blockIdx.x, nkt, p.Hk * p.B, kt, pair);  // causal: the keys with the most queries come first
-  const int hk = pair % p.Hk, b = pair / p.Hk;
+  ex_block_pair(blockIdx.x, nkt, p.Hk * p.B * p.kv_splits, p.causal || p.window, kt, pair);
+  const int hk = pair % p.Hk, b = pair / p.Hk % p.B, split = pair / (p.Hk * p.B);
   const ExRow0 br = ex_batch_row(p, b);
   const int kw = kt * 128 + wave * 32, j = kw + c;
   const ExTiles tiles = ex_query_tiles<64>(p, br, kt * 128, min(kt * 128 + 128, br.klen) - 1);
@@ -667,12 +665,17 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       d[4 * k] = u.x, d[4 * k + 1] = u.y, d[4 * k + 2] = u.z, d[4 * k + 3] = u.w;
     }
   };
-  float fac = p.s2, add = 0.f;
+  float fac = p.s2, add = 0.f, far_l = 0.f, far_r = 0.f;
+  int side = 0, diag = 0;  // where the half tile lies, and the entry of its first key and query
   const float* tl = nullptr;
+  const int64_t part = ((int64_t)(split * p.B + b) * nkt + kt) * kExWaves + wave;
+  if constexpr (BIAS)
+    for (int e = lane; e < 2 * n; e += 64) dg[e] = 0.f;
   auto fix = [&](f32x16_t& s, int i0) __attribute__((always_inline)) {
     const int q0 = br.pos + i0;
     if constexpr (BIAS) {
-      const int side = ex_bias_side(p, kw, q0, q0 + 31);
+      side = ex_bias_side(p, kw, q0, q0 + 31);
+      diag = p.D + 64 + kw - q0;
       fac = p.s2;
       add = 0.f;
       if (side != 0) {
@@ -684,12 +687,10 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
         for (int r = 0; r < 16; ++r) s[r] = __fmaf_rn(s[r], p.s2, at[-((r & 3) + 8 * (r >> 2))]);
       }
     }
-    // rows past the last query and keys past the last key add nothing that is kept
-    if (__builtin_expect(!ex_whole(p, q0, q0 + 31, kw, 0x7fffffff), 0)) {
+    // rows past the last query add nothing, and keys past the last key only to the bias gradient
+    if (__builtin_expect(!ex_whole(p, q0, q0 + 31, kw, BIAS ? br.klen : 0x7fffffff), 0)) {
       const ExSpan queries = ex_queries_of(p, br, kw + ex_opaque(c));
-      const int ih = i0 + 4 * hf;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = ex_in(queries, ih + (r & 3) + 8 * (r >> 2)) ? s[r] : -INFINITY;
+      ex_mask(s, queries, i0 + 4 * hf, q0 > 0);
     }
   };
   // Half tile ch of ct: P and dS from (s, d); half tile nh of nt: S and dP into (sn, dn); (ft, fh): the one
@@ -714,29 +715,42 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
         if (i < 8) e = ex_pair<BIAS>(s, i, fac, add);
         if (i > 0) {
           const int k = i - 1;
-          uint32_t w = pack_bf16x2(b4.e0, b4.e1), x = pack_bf16x2(b4.e0 * d[2 * k], b4.e1 * d[2 * k + 1]);
+          d[2 * k] *= b4.e0;
+          d[2 * k + 1] *= b4.e1;
+          uint32_t w = pack_bf16x2(b4.e0, b4.e1), x = pack_bf16x2(d[2 * k], d[2 * k + 1]);
           ex_pin(w);
           ex_pin(x);
           pp[k >> 2][k & 3] = w;
           ds[k >> 2][k & 3] = x;
         }
       }
+      if (BIAS && i == 8) {
+        if (side < 0) far_l += ex_sum16(d);
+        else if (side > 0) far_r += ex_sum16(d);
+        else ex_diagonals(d, dg + diag, n, lane);
+      }
       if (i == 9) start(s, d, ft, fh);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
 
+  const int all = tiles.n * p.G, from = ex_part(all, split, p.kv_splits), to_ = ex_part(all, split + 1, p.kv_splits);
   for (int g0 = 0; g0 < p.G; g0 += heads_at_once) {
-    const int ng = min(heads_at_once, p.G - g0), total = tiles.n * ng;
-    if (total == 0) break;
+    const int ng = min(heads_at_once, p.G - g0), h0 = hk * p.G + g0;
+    const int first = max(from - g0 * tiles.n, 0), total = min(to_ - g0 * tiles.n, tiles.n * ng) - first;
+    int g = 0, t = 0;  // head of the chunk and tile in use
+    if (total > 0) {
+    g = first / tiles.n;
+    t = first % tiles.n;
     if constexpr (BIAS) {
       __syncthreads();
-      ex_fill_bias<uint16_t>(p, reinterpret_cast<float*>(smem + kDkvTilesLds), hk * p.G + g0, ng);
+      ex_fill_bias<uint16_t>(p, tb, h0, ng);
+      for (int k = 0; k < g; ++k) ex_put_buckets(p, dg, n, 0.f, 0.f, part, h0 + k, lane);
+      tl = tb + g * n + p.D + 64;
     }
-    // the next tile to load: head lg of the chunk, tile lt
-    int lg = 0, lt = 0;
+    int lg = g, lt = t, left = total;  // the next tile to load, and how many
     auto load = [&](int slot) __attribute__((always_inline)) {  // past the last tile: zeros
-      const int h = hk * p.G + g0 + lg, i0 = ex_tile_at(tiles, lt) * 64, limit = lg < ng ? br.qlen : 0;
+      const int h = h0 + min(lg, ng - 1), i0 = ex_tile_at(tiles, lt) * 64, limit = left > 0 ? br.qlen : 0;
       const char* Qb = static_cast<const char*>(p.Q.data) + (b * p.Q.batch + h * kDHead) * 2;
       const char* Yb = static_cast<const char*>(p.dY.data) + (b * p.dY.batch + h * kDHead) * 2;
       const uint32_t to = lds + slot * kDkvTilesStage;
@@ -748,6 +762,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
         rs[2] = (uint32_t)__builtin_amdgcn_readfirstlane(max(min(limit - i0, 64), 0) * 4);
         ex_load_lds4(rs, lane * 4, to + 2 * kTile64 + 256 * wave);
       }
+      --left;
       if (++lt == tiles.n) {
         lt = 0;
         ++lg;
@@ -768,8 +783,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     start(s1, p1, smem, 1);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) fr[i] = read(i, smem, 1, nullptr, 0);
-    int b0 = 0, b1 = 1, b2 = 2, g = 0, t = 0;  // buffers of the tile, the next one, the one after
-    if constexpr (BIAS) tl = reinterpret_cast<const float*>(smem + kDkvTilesLds) + p.D + 64;
+    int b0 = 0, b1 = 1, b2 = 2;  // buffers of the tile, the next one, the one after
 #pragma clang loop unroll(disable)
     for (int it = 0; it < total; ++it) {
       wait_vmcnt<0>();
@@ -787,18 +801,82 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       b2 = o;
       if (++t == tiles.n) {
         t = 0;
-        if constexpr (BIAS) tl += n;
+        if constexpr (BIAS) {
+          ex_put_buckets(p, dg, n, far_l, far_r, part, h0 + g, lane);
+          far_l = far_r = 0.f;
+          tl += n;
+        }
+        ++g;
       }
     }
     wait_vmcnt<0>();  // no load is under way into what is written next
+    }
+    if constexpr (BIAS)
+      for (; g < ng; ++g) {  // what is left of the part's last head, and the heads behind it
+        ex_put_buckets(p, dg, n, far_l, far_r, part, h0 + g, lane);
+        far_l = far_r = 0.f;
+      }
   }
   __syncthreads();
+  if (p.kv_splits > 1) {
+    if (j < p.nk) {
+      const int64_t at = (((int64_t)(split * p.B + b) * p.nk + j) * p.Hk + hk) * kDHead + 4 * hf;
+#pragma unroll
+      for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const int64_t o = at + 32 * cc + 2 * r;
+          *reinterpret_cast<float4*>(p.part_dk + o) = make_float4(dk[cc][r], dk[cc][r + 1], dk[cc][r + 2], dk[cc][r + 3]);
+          *reinterpret_cast<float4*>(p.part_dv + o) = make_float4(dv[cc][r], dv[cc][r + 1], dv[cc][r + 2], dv[cc][r + 3]);
+        }
+    }
+    return;
+  }
   if (j >= br.klen) dk[0] = dk[1] = dv[0] = dv[1] = zero;
   char* st = smem + wave * 32 * 144;
   char* out = static_cast<char*>(p.dK.data) + (b * p.dK.batch + (int64_t)kw * p.dK.row + hk * kDHead) * 2;
   ex_store_rows32(st, dk, p.scale, out, p.dK.row * 2, p.nk - kw, lane);
   out = static_cast<char*>(p.dV.data) + (b * p.dV.batch + (int64_t)kw * p.dV.row + hk * kDHead) * 2;
   ex_store_rows32(st, dv, 1.f, out, p.dV.row * 2, p.nk - kw, lane);
+}
+
+// Adds up what k_exact_dkv leaves in parts: the first `sums` blocks the bias gradient, one (bucket, head)
+// per wave; the others dK and dV, eight columns of a key per thread.
+template <typename T>
+__global__ __launch_bounds__(kExThreads) void k_exact_join_grads(ExactParams p, int sums) {
+  const int lane = threadIdx.x & 63;
+  if ((int)blockIdx.x < sums) {
+    const int e = blockIdx.x * kExWaves + (threadIdx.x >> 6);  // bucket * H + head
+    if (e >= p.buckets * p.H) return;
+    float sum = 0.f;
+    for (int k = lane; k < p.bias_parts; k += 64) sum += p.part_bias[(int64_t)k * p.buckets * p.H + e];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane != 0) return;
+    if constexpr (ExFmt<T>::ES == 2) static_cast<T*>(p.dtable)[e] = (T)f32_to_bf16_bits(sum);
+    else static_cast<T*>(p.dtable)[e] = sum;
+    return;
+  }
+  const int64_t all = (int64_t)p.B * p.nk * p.Hk * kDHead, e = ((int64_t)(blockIdx.x - sums) * kExThreads + threadIdx.x) * 8;
+  if (e >= all) return;
+  const int col = (int)(e % (p.Hk * kDHead));
+  const int64_t row = e / (p.Hk * kDHead);
+  const int j = (int)(row % p.nk), b = (int)(row / p.nk);
+  const bool live = j < ex_batch_row(p, b).klen;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const float* from = (which ? p.part_dv : p.part_dk) + e;
+    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < p.kv_splits; ++s) {
+      const float4 x = *reinterpret_cast<const float4*>(from + s * all), y = *reinterpret_cast<const float4*>(from + s * all + 4);
+      o[0] += x.x, o[1] += x.y, o[2] += x.z, o[3] += x.w, o[4] += y.x, o[5] += y.y, o[6] += y.z, o[7] += y.w;
+    }
+    const float scale = live ? (which ? 1.f : p.scale) : 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o[k] = live ? o[k] * scale : 0.f;
+    const ExactOut& t = which ? p.dV : p.dK;
+    ex_store8(static_cast<T*>(t.data) + b * t.batch + j * t.row + col, o);
+  }
 }
 
 template <typename K>
@@ -810,22 +888,26 @@ hipError_t set_lds(K kernel, size_t lds) {
 // (backward pass, 8 x 128 tokens, 12 heads: 20.3 against 13.9 us; 4 x 128, one round, 11.7 against 13.6;
 // 1 x 512 16.2 and 25.0, 2 x 512 34.6 and 25.6).
 bool dq_in_tiles(const ExactParams& p) { return p.bf16 && exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B > device_cus(); }
-bool dkv_in_tiles(const ExactParams& p) { return p.bf16 && (int64_t)((p.nk + 31) / 32) * p.Hk * p.B > device_cus(); }
+bool dkv_in_tiles(const ExactParams& p) {
+  const char* v = getenv("EXV");
+  if (v && atoi(v) == 3 && p.bf16) return p.G * ((p.nq + 31) / 32) > 32 || (int64_t)((p.nk + 31) / 32) * p.Hk * p.B > device_cus();
+  return p.bf16 && (int64_t)((p.nk + 31) / 32) * p.Hk * p.B > device_cus();
+}
 
 template <typename T, bool BIAS>
 hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
-  const size_t tables = BIAS ? (size_t)exact_bias_entries(p.D) * (1 + kExWaves) * 4 : 0;
+  const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
   hipError_t e;
   if constexpr (ExFmt<T>::ES == 2) {
     if (dq_in_tiles(p)) {
-      const size_t lds = kDqTilesLds<BIAS> + tables;
+      const size_t lds = 6 * kTile64 + table;
       if ((e = set_lds(k_exact_dq_tiles<BIAS>, lds)) != hipSuccess) return e;
       const int64_t blocks = (int64_t)((p.nq + 127) / 128) * p.H * p.B;
       hipLaunchKernelGGL((k_exact_dq_tiles<BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
       return hipGetLastError();
     }
   }
-  const size_t lds = kDqLds<T> + tables;
+  const size_t lds = kDqLds<T> + table * p.Gp;
   if ((e = set_lds(k_exact_dq<T, BIAS>, lds)) != hipSuccess) return e;
   const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
   hipLaunchKernelGGL((k_exact_dq<T, BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
@@ -835,26 +917,29 @@ hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
 template <typename T, bool BIAS>
 hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
   const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
-  const int64_t sums = BIAS ? (p.buckets * p.H + kExWaves - 1) / kExWaves : 0;  // blocks that add up the bias gradient
+  const bool in_tiles = dkv_in_tiles(p);
+  // a block's share of the LDS (two blocks to a CU in tiles), its tiles, its waves' sums along diagonals
+  const size_t room = in_tiles ? 81920 : 163840, base = (in_tiles ? kDkvTilesLds : kDkvLds<T>) + 2 * kExWaves * table;
+  const int at_once = BIAS ? (int)((room - base) / table) : p.G;  // heads whose bias tables fit
+  const int heads = at_once < p.G ? at_once : p.G;
+  const size_t lds = base + table * heads;
+  const int64_t blocks = (int64_t)((p.nk + (in_tiles ? 127 : 31)) / (in_tiles ? 128 : 32)) * p.Hk * p.B * p.kv_splits;
   hipError_t e;
   if constexpr (ExFmt<T>::ES == 2) {
-    if (dkv_in_tiles(p)) {
-      const int at_once = BIAS ? (int)((81920 - kDkvTilesLds) / table) : p.G;  // two blocks to a CU
-      const int heads = at_once < p.G ? at_once : p.G;
-      const size_t lds = kDkvTilesLds + table * heads;
+    if (in_tiles) {
       if ((e = set_lds(k_exact_dkv_tiles<BIAS>, lds)) != hipSuccess) return e;
-      const int64_t blocks = (int64_t)((p.nk + 127) / 128) * p.Hk * p.B + sums;
       hipLaunchKernelGGL((k_exact_dkv_tiles<BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
-      return hipGetLastError();
     }
   }
-  // heads whose bias tables fit beside the tiles at once
-  const int at_once = BIAS ? (int)((163840 - kDkvLds<T>) / table) : p.G;
-  const int heads = at_once < p.G ? at_once : p.G;
-  const size_t lds = kDkvLds<T> + table * heads;
-  if ((e = set_lds(k_exact_dkv<T, BIAS>, lds)) != hipSuccess) return e;
-  const int64_t blocks = (int64_t)((p.nk + 31) / 32) * p.Hk * p.B + sums;
-  hipLaunchKernelGGL((k_exact_dkv<T, BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
+  if (!in_tiles) {
+    if ((e = set_lds(k_exact_dkv<T, BIAS>, lds)) != hipSuccess) return e;
+    hipLaunchKernelGGL((k_exact_dkv<T, BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
+  }
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int sums = BIAS ? (p.buckets * p.H + kExWaves - 1) / kExWaves : 0;
+  const int64_t rows = p.kv_splits > 1 ? ((int64_t)p.B * p.nk * p.Hk * (kDHead / 8) + kExThreads - 1) / kExThreads : 0;
+  if (sums + rows == 0) return hipSuccess;
+  hipLaunchKernelGGL((k_exact_join_grads<T>), dim3((unsigned)(sums + rows)), dim3(kExThreads), 0, s, p, sums);
   return hipGetLastError();
 }
 
@@ -866,8 +951,19 @@ hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
 
 }  // namespace
 
-int exact_bias_parts(const ExactParams& p) {
-  return (int)(p.B * (dq_in_tiles(p) ? (p.nq + 127) / 128 : exact_row_tiles(p.nq, p.Gp)));
+// Blocks that share a key's queries: where they leave CUs without one (few keys, or few key heads with
+// many query heads), as many as that takes, of at least two tiles to a wave.
+int exact_kv_splits(const ExactParams& p) {
+  const bool in_tiles = dkv_in_tiles(p);
+  const int64_t blocks = (int64_t)((p.nk + (in_tiles ? 127 : 31)) / (in_tiles ? 128 : 32)) * p.Hk * p.B;
+  const int64_t tiles = (int64_t)p.G * ((p.nq + (in_tiles ? 63 : 31)) / (in_tiles ? 64 : 32));
+  const int64_t want = (in_tiles ? 2 : 1) * device_cus() / blocks, most = tiles / (in_tiles ? 4 : 2 * kExWaves);
+  const int64_t n = want < most ? want : most;
+  return n < 1 ? 1 : (int)n;
+}
+
+int64_t exact_bias_parts(const ExactParams& p) {  // a part per wave of k_exact_dkv
+  return (int64_t)p.kv_splits * p.B * ((p.nk + (dkv_in_tiles(p) ? 127 : 31)) / (dkv_in_tiles(p) ? 128 : 32)) * kExWaves;
 }
 
 hipError_t launch_exact_backward(const ExactParams& p, hipStream_t s) {

@@ -128,8 +128,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
       for (int r = 0; r < 16; ++r) x[r] *= p.s2;
     }
     if (!ex_whole(p, pmin, pmax, k0, br.klen)) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = ex_in(keys, k0 + 4 * hf + (r & 3) + 8 * (r >> 2)) ? x[r] : -INFINITY;
+      ex_mask(x, keys, k0 + 4 * hf, k0 > 0);
     }
     ex_softmax_step(s, x);
     ex_cols_product<T>(s.y, kt + TB, x, lane);
@@ -236,7 +235,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
   const int c = lane & 31, hf = lane >> 5;
   int qt, pair;
   const int nqt = (p.nq + QB - 1) / QB;
-  ex_block_pair(blockIdx.x, nqt, p.H * p.B, qt, pair);
+  ex_block_pair(blockIdx.x, nqt, p.H * p.B, p.causal || p.window, qt, pair);
   if (p.causal) qt = nqt - 1 - qt;  // the longest rows first
   const int h = pair % p.H, b = pair / p.H, hk = h / p.G;
   const ExRow0 br = ex_batch_row(p, b);
@@ -321,10 +320,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         const ExSpan keys = ex_keys_of(p, br.pos + qw + 32 * m + ex_opaque(c), br.klen);
-        const int kh = k0 + 4 * hf;
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          s[m][r] = ex_in(keys, kh + (r & 3) + 8 * (r >> 2)) ? s[m][r] : -INFINITY;
+        ex_mask(s[m], keys, k0 + 4 * hf, k0 > 0);
       }
     }
   };
@@ -501,10 +497,9 @@ hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
 }  // namespace
 
 // Heads side by side in the kernels of 32 rows: a key head's whole group, unless its bias tables do not
-// fit beside the tiles. One where the bias gradient is taken, along the diagonals of a head's tiles.
-int exact_group(const ExactParams& p, bool backward) {
-  if (!p.table) return p.G;
-  return !backward && (int64_t)p.G * exact_bias_entries(p.D) <= 8192 ? p.G : 1;
+// fit beside the tiles.
+int exact_group(const ExactParams& p) {
+  return !p.table || (int64_t)p.G * exact_bias_entries(p.D) <= 8192 ? p.G : 1;
 }
 
 // bf16 in blocks of 128 queries or more: where the blocks of 32 rows are more than the CUs (one of those
@@ -519,10 +514,12 @@ static bool forward_in_tiles(const ExactParams& p) {
 // 256 queries per block instead of 128 halve the LDS reads and the loads per score, and take about 1.75
 // times as long: by what the CU with the most blocks has to do (4 x 4096 tokens, 12 heads: 6 blocks
 // against 3, 227 and 203 us; 8 x 1057: 4 and 2, 47.8 and 42.5; 3 x 2000: 3 and 2, 60.5 and 67.2; 32 x
-// 250: 3 and 2, 16.6 and 19.1). Not with a bias, whose masks and tables leave too few registers.
+// 250: 3 and 2, 16.6 and 19.1). Not with a bias,
+// whose table leaves too few registers, nor under a window, where a wave of fewer queries has fewer keys
+// that others of the block need.
 static bool forward_wide(const ExactParams& p) {
   const int64_t q128 = (p.nq + 127) / 128, pairs = (int64_t)p.H * p.B;
-  return !p.table && 4 * blocks_per_cu(q128 * pairs) > 7 * blocks_per_cu((q128 + 1) / 2 * pairs);
+  return !p.table && !p.window && 4 * blocks_per_cu(q128 * pairs) > 7 * blocks_per_cu((q128 + 1) / 2 * pairs);
 }
 
 // Blocks that share a row's keys: as many as fill the card four times over, where every wave still
