@@ -55,6 +55,11 @@ inline int exact_bias_entries(int D) { return 2 * D + 129; }  // rel = j - p in 
 // Rows (query, head) that the kernels of 32 rows pad to.
 inline int64_t exact_row_tiles(int64_t nq, int64_t Gp) { return (nq * Gp + 31) / 32; }
 
+// Whether `tiles` of 32 over four waves are worth splitting into n parts: what that saves in tiles one after
+// another, each `unit` times 0.55 us, against the 3 us of the launch that joins them.
+inline bool exact_worth(int64_t tiles, int64_t n, int unit) {
+  return ((tiles + 3) / 4 - (tiles + 4 * n - 1) / (4 * n)) * unit >= 6;
+}
 int exact_splits(const ExactParams& p);
 int exact_kv_splits(const ExactParams& p);
 int64_t exact_bias_parts(const ExactParams& p);

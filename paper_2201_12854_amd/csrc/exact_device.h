@@ -83,6 +83,13 @@ __device__ __forceinline__ void ex_load_tile(u32x4_t rs, int pitch, uint32_t lds
   }
 }
 
+// x, which the compiler can neither foresee nor move: what a rare branch computes from it is not kept
+// in registers outside of the branch.
+__device__ __forceinline__ int ex_opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // ------------------------------------------------------------------ operands and products
 template <typename T> struct ExRow { u32x4_t v[ExFmt<T>::NG]; };  // a lane's half of a row
 
@@ -162,12 +169,13 @@ __device__ __forceinline__ void ex_cols_product(f32x16_t (&y)[2], const char* ti
       }
     }
   } else {
+    const int ln = ex_opaque(lane), h4 = (ln >> 5) * 4;  // 32 addresses, taken anew rather than kept in registers
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int row = (r & 3) + 8 * (r >> 2) + 4 * hf;
+      const int row = (r & 3) + 8 * (r >> 2) + h4;
 #pragma unroll
       for (int cc = 0; cc < 2; ++cc) {
-        const int col = 32 * cc + (lane & 31);
+        const int col = 32 * cc + (ln & 31);
         const float a =
             *reinterpret_cast<const float*>(tile + row * 256 + (((col >> 2) ^ ex_swz<T>(row)) << 4) + (col & 3) * 4);
         y[cc] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, x[r], y[cc], 0, 0, 0);
@@ -188,10 +196,31 @@ __device__ __forceinline__ uint32_t ex_load64(int wave, int lane, int pitch) {
   const int row = 8 * wave + (lane >> 3);
   return (uint32_t)(row * pitch + (((lane & 7) ^ (COLS ? ex_swz_cols(row) : ex_swz<uint16_t>(row))) << 4));
 }
-__device__ __forceinline__ void ex_load_tile64(const char* base, int pitch, int row0, int limit, uint32_t off, uint32_t lds,
-                                               int wave) {
-  ex_load_lds16(ex_rsrc(base, pitch, row0, limit, 128), off, lds + 1024u * wave);
-  ex_load_lds16(ex_rsrc(base, pitch, row0 + 32, limit, 128), off, lds + 4096u + 1024u * wave);
+// The tiles of a matrix that a block loads one after another: where the next one begins and how many
+// rows there are from there on, in scalar registers (few scalar instructions per tile: where a SIMD
+// has one wave, every instruction costs it about five cycles).
+struct ExStream {
+  const char* at;
+  int rows;
+};
+__device__ __forceinline__ ExStream ex_stream(const char* base, int pitch, int row0, int limit) {
+  return ExStream{base + (int64_t)row0 * pitch, limit - row0};
+}
+__device__ __forceinline__ void ex_load_next64(ExStream& m, int pitch, uint32_t off, uint32_t lds, int wave) {
+  const int half = 32 * pitch, bytes = max((min(m.rows, 64) - 1) * pitch + 128, 0);
+  auto words = [](const char* p, int n) __attribute__((always_inline)) {
+    const uint64_t a = (uint64_t)(uintptr_t)p;
+    u32x4_t w;
+    w[0] = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+    w[1] = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu));
+    w[2] = (uint32_t)__builtin_amdgcn_readfirstlane(n);
+    w[3] = 0x00020000u;
+    return w;
+  };
+  ex_load_lds16(words(m.at, bytes), off, lds + 1024u * wave);
+  ex_load_lds16(words(m.at + half, max(bytes - half, 0)), off, lds + 4096u + 1024u * wave);
+  m.at += 2 * (int64_t)half;
+  m.rows -= 64;
 }
 
 // The lane's byte addresses in a tile: row c, chunks 2 g + hf; and the transposing reads of rows
@@ -262,13 +291,6 @@ __device__ __forceinline__ void ex_store_rows32(char* st, const f32x16_t (&y)[2]
 // Keeps the computation of x before this point and what follows behind it.
 template <typename T>
 __device__ __forceinline__ void ex_pin(T& x) { asm volatile("" : "+v"(x)); }
-
-// x, which the compiler can neither foresee nor move: what a rare branch computes from it is not kept
-// in registers outside of the branch.
-__device__ __forceinline__ int ex_opaque(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
 
 // The rows tile and (batch row, head) `pair` of block `bid`: the tiles of a pair on one XCD where the pairs
 // come in eights. `uneven`: every pair's tile 0 before any tile 1, where a mask makes some tiles far
@@ -409,6 +431,25 @@ __device__ __forceinline__ bool ex_whole(const ExactParams& p, int pmin, int pma
   return w;
 }
 
+// The same as a range: of first keys k0 for queries at pmin .. pmax, and of first positions q0 of 32 queries
+// for the keys j0 .. j0 + 31 (none where those pass klen).
+struct ExRange {
+  int lo, hi;
+};
+__device__ __forceinline__ bool ex_has(const ExRange& r, int x) { return x >= r.lo && x <= r.hi; }
+__device__ __forceinline__ ExRange ex_whole_keys(const ExactParams& p, int pmin, int pmax, int klen) {
+  ExRange r{-0x40000000, klen - 32};
+  if (p.causal) r.hi = min(r.hi, pmin - 31);
+  if (p.window) r = ExRange{pmax - p.half, min(r.hi, pmin + p.half - 31)};
+  return r;
+}
+__device__ __forceinline__ ExRange ex_whole_queries(const ExactParams& p, int j0, int klen) {
+  ExRange r{-0x40000000, j0 + 32 <= klen ? 0x40000000 : -0x40000001};
+  if (p.causal) r.lo = j0 + 31;
+  if (p.window) r = ExRange{max(r.lo, j0 + 31 - p.half), min(r.hi, j0 + p.half - 31)};
+  return r;
+}
+
 // ------------------------------------------------------------------ relative bias
 // Bucket of the key rel = j - p places behind the query: distances below E have one each, distance
 // d >= E the bucket E + (number of thresholds <= d); the buckets of rel > 0 follow those of rel <= 0.
@@ -430,7 +471,7 @@ __device__ __forceinline__ float ex_elem(const void* base, int64_t i) {
 template <typename T>
 __device__ __forceinline__ void ex_fill_bias(const ExactParams& p, float* tb, int h0, int nh) {
   const int n = 2 * p.D + 129;
-  for (int e = threadIdx.x; e < n; e += kExThreads) {
+  for (int e = threadIdx.x; e < n; e += blockDim.x) {
     const int c = ex_bucket(p, min(max(e - p.D - 64, -p.D), p.D));
     for (int g = 0; g < nh; ++g) {
       const float v = ex_elem<T>(p.table, (int64_t)c * p.H + h0 + g);

@@ -6,29 +6,25 @@
 // the query heads that share them; also the bias gradient). That takes S and dP twice: seven
 // products for the five that the formulas need. k_exact_join_grads adds up what the blocks of
 // k_exact_dkv leave in parts.
-#include <cstdlib>
+#include <algorithm>
+
 #include "exact_device.h"
 #include "mca_kernels.h"
 
 namespace mca {
 namespace {
 
-template <typename T> constexpr int kBwdStages = ExFmt<T>::ES == 2 ? 3 : 2;
+template <typename T> constexpr int kBwdStages = ExFmt<T>::ES == 2 ? 2 : 1;
 template <typename T> constexpr int kDqLds = kExWaves * kBwdStages<T> * 2 * tile_bytes<T>();
 template <typename T> constexpr int kDkvStage = 2 * tile_bytes<T>() + 512;  // Q, dY, two planes of statistics
 template <typename T> constexpr int kDkvLds = kExWaves * kBwdStages<T> * kDkvStage<T>;
 constexpr int kYS = kDHead + 4;  // row pitch of the sums that the waves of a block join in LDS
 
-// Eight consecutive values of a row to `o`.
+// Four consecutive values of a row to `o`.
 template <typename T>
-__device__ __forceinline__ void ex_store8(T* o, const float (&y)[8]) {
-  if constexpr (ExFmt<T>::ES == 2) {
-    *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]),
-                                              pack_bf16x2(y[6], y[7]));
-  } else {
-    reinterpret_cast<float4*>(o)[0] = make_float4(y[0], y[1], y[2], y[3]);
-    reinterpret_cast<float4*>(o)[1] = make_float4(y[4], y[5], y[6], y[7]);
-  }
+__device__ __forceinline__ void ex_store4(T* o, float4 y) {
+  if constexpr (ExFmt<T>::ES == 2) *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
+  else *reinterpret_cast<float4*>(o) = y;
 }
 __device__ __forceinline__ void ex_put_sums(float* ys, const f32x16_t (&y)[2], int row, int hf) {
 #pragma unroll
@@ -38,14 +34,15 @@ __device__ __forceinline__ void ex_put_sums(float* ys, const f32x16_t (&y)[2], i
       *reinterpret_cast<float4*>(ys + row * kYS + 32 * cc + 8 * (r >> 2) + 4 * hf) =
           make_float4(y[cc][r], y[cc][r + 1], y[cc][r + 2], y[cc][r + 3]);
 }
-__device__ __forceinline__ void ex_join_sums(float (&o)[8], const float* ys, int row, int col, float scale) {
+// Four columns of a row, summed over the waves in their order.
+__device__ __forceinline__ float4 ex_join_sums(const float* ys, int row, int col, float scale) {
+  float4 v = *reinterpret_cast<const float4*>(ys + row * kYS + col);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float v = ys[row * kYS + col + e];
-#pragma unroll
-    for (int k = 1; k < kExWaves; ++k) v += ys[(k * 32 + row) * kYS + col + e];
-    o[e] = v * scale;
+  for (int k = 1; k < kExWaves; ++k) {
+    const float4 t = *reinterpret_cast<const float4*>(ys + (k * 32 + row) * kYS + col);
+    v.x += t.x, v.y += t.y, v.z += t.z, v.w += t.w;
   }
+  return make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
 }
 
 // What k_exact_dkv starts from.
@@ -73,10 +70,11 @@ __device__ __forceinline__ float ex_shift_rows(float v) {  // only the rows of 1
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), CTRL,
                                                                ROWS, 0xF, true));
 }
-// Adds a tile's sums to a wave's two arrays of n entries: `at` is the entry of rel = key 0 - query 0.
-__device__ __forceinline__ void ex_diagonals(const f32x16_t& x, float* at, int n, int lane) {
+// Adds a tile's sums to a wave's array: `at` is the entry of rel = key 0 - query 0.
+__device__ __forceinline__ void ex_diagonals(const f32x16_t& x, float* at, int lane_) {
+  const int lane = ex_opaque(lane_);
   const int a = (lane >> 4) & 1, f = lane & 15;
-  float* o = at + (lane < 32 ? f - 15 : n + f) + 16 * a;
+  float* o = at + (lane < 32 ? f - 15 : f) + 16 * a;
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {  // queries 16 kb + {0 .. 3, 8 .. 11} + 4 hf
     float up = x[8 * kb], down = x[8 * kb + 7];
@@ -91,27 +89,24 @@ __device__ __forceinline__ void ex_diagonals(const f32x16_t& x, float* at, int n
     const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(up), __float_as_uint(down), false, false);
     const float v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
     wave_lds_sync();
-    o[-16 * kb] += lane >= 32 && f == 0 ? 0.f : v;
+    if (lane < 32) o[-16 * kb] += v;  // the two halves' entries overlap
+    wave_lds_sync();
+    if (lane >= 32 && f > 0) o[-16 * kb] += v;
   }
   wave_lds_sync();
 }
 // Takes a wave's sums of a head out as a part of the bias gradient: far tiles' sums per lane (`left`: rel
-// <= -D, `right`: rel >= D) and the two arrays, which are left as zeros. A bucket's entries are neighbours;
-// four lanes share those of a bucket.
+// <= -D, `right`: rel >= D) and the array, which is left as zeros. A bucket's entries are neighbours; four
+// lanes share those of a bucket.
 __device__ __forceinline__ void ex_put_buckets(const ExactParams& p, float* dg, int n, float left, float right, int64_t part,
-                                               int head, int lane) {
+                                               int head, int lane_) {
+  const int lane = ex_opaque(lane_);
   wave_lds_sync();
   left += ex_other_half(left);
   right += ex_other_half(right);
   if (lane < 32) {  // entries of the far sides, one per lane
     dg[lane] += left;
     dg[n - 1 - lane] += right;
-  }
-  wave_lds_sync();
-#pragma unroll 4
-  for (int e = lane; e < n; e += 64) {
-    dg[e] += dg[n + e];
-    dg[n + e] = 0.f;
   }
   wave_lds_sync();
   const int far = p.D + 64;
@@ -146,7 +141,7 @@ __device__ __forceinline__ float ex_sum16(const T& x) {
 }
 
 // ------------------------------------------------------------------ dQ
-// Blocks of 32 (query, head) rows whose key tiles the four waves share, as k_exact_rows. S^T = K Q^T
+// Blocks of 32 (query, head) rows whose key tiles the waves share, as k_exact_rows. S^T = K Q^T
 // and dP^T = V dY^T: the row's c and D are one value per lane, and dS feeds dQ^T = K^T dS^T.
 //
 //
@@ -267,20 +262,22 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
   }
   __syncthreads();
   if (wave == 0 && hf == 0 && i < p.nq) {
-    if constexpr (BIAS && ES == 2) D += rests[c] + rests[32 + c] + rests[64 + c] + rests[96 + c];
+    if constexpr (BIAS && ES == 2)
+      for (int k = 0; k < kExWaves; ++k) D += rests[k * 32 + c];
     ex_put_stat<T>(p, ((int64_t)b * p.H + head) * p.nq + i, cr, D);
   }
-  const int row = threadIdx.x >> 3, col = (threadIdx.x & 7) * 8;
-  const int vr = vt * 32 + row, ir = vr / p.Gp;
-  if (ir < p.nq) {
-    float o[8];
-    ex_join_sums(o, ys, row, col, p.scale);
-    ex_store8(static_cast<T*>(p.dQ.data) + b * p.dQ.batch + ir * p.dQ.row + (hx * p.Gp + vr % p.Gp) * kDHead + col, o);
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int row = (threadIdx.x >> 4) + half * 16, col = (threadIdx.x & 15) * 4;
+    const int vr = vt * 32 + row, ir = vr / p.Gp;
+    if (ir < p.nq)
+      ex_store4(static_cast<T*>(p.dQ.data) + b * p.dQ.batch + ir * p.dQ.row + (hx * p.Gp + vr % p.Gp) * kDHead + col,
+                ex_join_sums(ys, row, col, p.scale));
   }
 }
 
 // ------------------------------------------------------------------ dK, dV
-// Blocks of 32 keys of a key head; the four waves share the query tiles of all its query heads, or of the
+// Blocks of 32 keys of a key head; the waves share the query tiles of all its query heads, or of the
 // block's part of them (kv_splits). S = Q K^T and dP = dY V^T with the lane holding a key: P and dS
 // feed dV^T = dY^T P and dK^T = Q^T dS. A wave loads its tiles of Q, dY and row statistics straight
 // into LDS.
@@ -292,8 +289,8 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
   const int nkt = (p.nk + 31) / 32;
   int bid = blockIdx.x;
   const int c = lane & 31, hf = lane >> 5, n = 2 * p.D + 129;
-  float* dg = reinterpret_cast<float*>(smem + kDkvLds<T>) + wave * 2 * n;  // the wave's sums along diagonals
-  float* tb = reinterpret_cast<float*>(smem + kDkvLds<T>) + kExWaves * 2 * n;  // [heads_at_once][n]
+  float* dg = reinterpret_cast<float*>(smem + kDkvLds<T>) + wave * n;  // the wave's sums along diagonals
+  float* tb = reinterpret_cast<float*>(smem + kDkvLds<T>) + kExWaves * n;  // [heads_at_once][n]
   const int kt = bid % nkt;
   bid /= nkt;
   const int hk = bid % p.Hk;
@@ -315,7 +312,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
   float far_l = 0.f, far_r = 0.f;
   const int64_t part = ((int64_t)(split * p.B + b) * nkt + kt) * kExWaves + wave;
   if constexpr (BIAS)
-    for (int e = lane; e < 2 * n; e += 64) dg[e] = 0.f;
+    for (int e = lane; e < n; e += 64) dg[e] = 0.f;
 
   for (int g0 = 0; g0 < p.G; g0 += heads_at_once) {
     const int ng = min(heads_at_once, p.G - g0), h0 = hk * p.G + g0;
@@ -364,8 +361,11 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
         for (int r = 0; r < 16; ++r) {
           x[r] += cr[r];
           ds[r] += D[r];
-          cr[r] = D[r] = 0.f;
+          cr[r] = 0.f;
         }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ds[r] -= D[r];
       }
       int side = 0;
       if constexpr (BIAS) {
@@ -395,14 +395,14 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         x[r] = ex_exp2(x[r]);
-        ds[r] = x[r] * (ds[r] - D[r]);
+        ds[r] *= x[r];
       }
       ex_cols_product<T>(dv, qt + TB, x, lane);
       ex_cols_product<T>(dk, qt, ds, lane);
       if constexpr (BIAS) {
         if (side < 0) far_l += ex_sum16(ds);
         else if (side > 0) far_r += ex_sum16(ds);
-        else ex_diagonals(ds, dg + p.D + 64 + kt * 32 - p0, n, lane);
+        else ex_diagonals(ds, dg + p.D + 64 + kt * 32 - p0, lane);
       }
       slot = slot == ST - 1 ? 0 : slot + 1;
     }
@@ -414,26 +414,27 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
     wait_vmcnt<0>();
   }
   __syncthreads();
-  float* ys = reinterpret_cast<float*>(smem);
-  ex_put_sums(ys, dk, wave * 32 + c, hf);
-  ex_put_sums(ys + kExWaves * 32 * kYS, dv, wave * 32 + c, hf);
-  __syncthreads();
-  const int row = threadIdx.x >> 3, col = (threadIdx.x & 7) * 8, jr = kt * 32 + row;
-  if (jr >= p.nk) return;
-  if (p.kv_splits > 1) {
-    float o[8];
-    const int64_t at = (((int64_t)(split * p.B + b) * p.nk + jr) * p.Hk + hk) * kDHead + col;
-    ex_join_sums(o, ys, row, col, 1.f);
-    ex_store8(p.part_dk + at, o);
-    ex_join_sums(o, ys + kExWaves * 32 * kYS, row, col, 1.f);
-    ex_store8(p.part_dv + at, o);
-    return;
+  float* ys = reinterpret_cast<float*>(smem);  // one of the two at a time
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if (which) __syncthreads();
+    ex_put_sums(ys, which ? dv : dk, wave * 32 + c, hf);
+    __syncthreads();
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int row = (threadIdx.x >> 4) + half * 16, col = (threadIdx.x & 15) * 4, jr = kt * 32 + row;
+      if (jr >= p.nk) continue;
+      if (p.kv_splits > 1) {
+        const int64_t at = (((int64_t)(split * p.B + b) * p.nk + jr) * p.Hk + hk) * kDHead + col;
+        ex_store4((which ? p.part_dv : p.part_dk) + at, ex_join_sums(ys, row, col, 1.f));
+      } else {
+        const ExactOut& t = which ? p.dV : p.dK;
+        const float4 v = ex_join_sums(ys, row, col, which ? 1.f : p.scale);
+        ex_store4(static_cast<T*>(t.data) + b * t.batch + jr * t.row + hk * kDHead + col,
+                  jr < br.klen ? v : make_float4(0.f, 0.f, 0.f, 0.f));
+      }
+    }
   }
-  float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (jr < br.klen) ex_join_sums(o, ys, row, col, p.scale);
-  ex_store8(static_cast<T*>(p.dK.data) + b * p.dK.batch + jr * p.dK.row + hk * kDHead + col, o);
-  if (jr < br.klen) ex_join_sums(o, ys + kExWaves * 32 * kYS, row, col, 1.f);
-  ex_store8(static_cast<T*>(p.dV.data) + b * p.dV.batch + jr * p.dV.row + hk * kDHead + col, o);
 }
 
 // ------------------------------------------------------------------ tiles of 64 rows, bf16
@@ -477,16 +478,22 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   const int qw = qt * 128 + wave * 32, i = qw + c;
   const int last = min(qt * 128 + 128, br.qlen) - 1;
   const ExTiles tiles = last >= qt * 128 ? ex_key_tiles<64>(p, br.pos + qt * 128, br.pos + last, br.klen) : ExTiles{-1, 0, 0};
-  const int wmin = br.pos + qw, wmax = br.pos + min(qw + 32, br.qlen) - 1;
+  const ExRange whole = ex_whole_keys(p, br.pos + qw, br.pos + min(qw + 32, br.qlen) - 1, br.klen);
 
   const char* Kb = static_cast<const char*>(p.K.data) + (b * p.K.batch + hk * kDHead) * 2;
   const char* Vb = static_cast<const char*>(p.V.data) + (b * p.V.batch + hk * kDHead) * 2;
   const int kpitch = (int)p.K.row * 2, vpitch = (int)p.V.row * 2;
   const uint32_t kl = ex_load64(wave, lane, kpitch), vl = ex_load64(wave, lane, vpitch), lds = lds_addr(smem);
-  auto load = [&](int t, int slot) __attribute__((always_inline)) {  // past the last tile: zeros
-    const int k0 = ex_tile_at(tiles, t) * 64, limit = t < tiles.n ? br.klen : 0;
-    ex_load_tile64(Kb, kpitch, k0, limit, kl, lds + slot * kTile64, wave);
-    ex_load_tile64(Vb, vpitch, k0, limit, vl, lds + (3 + slot) * kTile64, wave);
+  // Tile t into buffer `slot`, in the order of t; past the last tile: zeros
+  ExStream ks, vs;
+  auto load = [&](int t, int slot) __attribute__((always_inline)) {
+    if (t == 0 || (tiles.first >= 0 && t == 1)) {
+      ks = ex_stream(Kb, kpitch, ex_tile_at(tiles, t) * 64, br.klen);
+      vs = ex_stream(Vb, vpitch, ex_tile_at(tiles, t) * 64, br.klen);
+    }
+    if (t >= tiles.n) ks.rows = vs.rows = 0;
+    ex_load_next64(ks, kpitch, kl, lds + slot * kTile64, wave);
+    ex_load_next64(vs, vpitch, vl, lds + (3 + slot) * kTile64, wave);
   };
   load(0, 0);
   const bool live = i < br.qlen;
@@ -546,7 +553,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
         for (int r = 0; r < 16; ++r) s[r] = __fmaf_rn(s[r], p.s2, at[(r & 3) + 8 * (r >> 2)]);
       }
     }
-    if (__builtin_expect(!ex_whole(p, wmin, wmax, k0, br.klen), 0)) {
+    if (__builtin_expect(!ex_has(whole, k0), 0)) {
       const ExSpan keys = ex_keys_of(p, br.pos + qw + ex_opaque(c), br.klen);
       ex_mask(s, keys, k0 + 4 * hf, k0 > 0);
     }
@@ -628,8 +635,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hf = lane >> 5, n = 2 * p.D + 129;
   const int nkt = (p.nk + 127) / 128;
-  float* dg = reinterpret_cast<float*>(smem + kDkvTilesLds) + wave * 2 * n;
-  float* tb = reinterpret_cast<float*>(smem + kDkvTilesLds) + kExWaves * 2 * n;
+  float* dg = reinterpret_cast<float*>(smem + kDkvTilesLds) + wave * n;
+  float* tb = reinterpret_cast<float*>(smem + kDkvTilesLds) + kExWaves * n;
   int kt, pair;
   ex_block_pair(blockIdx.x, nkt, p.Hk * p.B * p.kv_splits, p.causal || p.window, kt, pair);
   const int hk = pair % p.Hk, b = pair / p.Hk % p.B, split = pair / (p.Hk * p.B);
@@ -665,12 +672,13 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       d[4 * k] = u.x, d[4 * k + 1] = u.y, d[4 * k + 2] = u.z, d[4 * k + 3] = u.w;
     }
   };
+  const ExRange whole = ex_whole_queries(p, kw, BIAS ? br.klen : 0x7fffffff);
   float fac = p.s2, add = 0.f, far_l = 0.f, far_r = 0.f;
   int side = 0, diag = 0;  // where the half tile lies, and the entry of its first key and query
   const float* tl = nullptr;
   const int64_t part = ((int64_t)(split * p.B + b) * nkt + kt) * kExWaves + wave;
   if constexpr (BIAS)
-    for (int e = lane; e < 2 * n; e += 64) dg[e] = 0.f;
+    for (int e = lane; e < n; e += 64) dg[e] = 0.f;
   auto fix = [&](f32x16_t& s, int i0) __attribute__((always_inline)) {
     const int q0 = br.pos + i0;
     if constexpr (BIAS) {
@@ -688,7 +696,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       }
     }
     // rows past the last query add nothing, and keys past the last key only to the bias gradient
-    if (__builtin_expect(!ex_whole(p, q0, q0 + 31, kw, BIAS ? br.klen : 0x7fffffff), 0)) {
+    if (__builtin_expect(!ex_has(whole, q0), 0)) {
       const ExSpan queries = ex_queries_of(p, br, kw + ex_opaque(c));
       ex_mask(s, queries, i0 + 4 * hf, q0 > 0);
     }
@@ -727,7 +735,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       if (BIAS && i == 8) {
         if (side < 0) far_l += ex_sum16(d);
         else if (side > 0) far_r += ex_sum16(d);
-        else ex_diagonals(d, dg + diag, n, lane);
+        else ex_diagonals(d, dg + diag, lane);
       }
       if (i == 9) start(s, d, ft, fh);
       __builtin_amdgcn_sched_barrier(0);
@@ -748,22 +756,36 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       for (int k = 0; k < g; ++k) ex_put_buckets(p, dg, n, 0.f, 0.f, part, h0 + k, lane);
       tl = tb + g * n + p.D + 64;
     }
-    int lg = g, lt = t, left = total;  // the next tile to load, and how many
+    // the next tile to load (head lg, tile lt), and how many
+    int lg = g, lt = t, left = total;
+    bool jump = true;
+    ExStream qs, ys;
+    const char* stat = nullptr;  // of the wave's plane, for the tile
     auto load = [&](int slot) __attribute__((always_inline)) {  // past the last tile: zeros
-      const int h = h0 + min(lg, ng - 1), i0 = ex_tile_at(tiles, lt) * 64, limit = left > 0 ? br.qlen : 0;
-      const char* Qb = static_cast<const char*>(p.Q.data) + (b * p.Q.batch + h * kDHead) * 2;
-      const char* Yb = static_cast<const char*>(p.dY.data) + (b * p.dY.batch + h * kDHead) * 2;
+      if (jump) {
+        const int h = h0 + min(lg, ng - 1), i0 = ex_tile_at(tiles, lt) * 64;
+        qs = ex_stream(static_cast<const char*>(p.Q.data) + (b * p.Q.batch + h * kDHead) * 2, qpitch, i0, br.qlen);
+        ys = ex_stream(static_cast<const char*>(p.dY.data) + (b * p.dY.batch + h * kDHead) * 2, ypitch, i0, br.qlen);
+        stat = reinterpret_cast<const char*>(p.rowstat + ((int64_t)(wave & 1) * p.B * p.H + (int64_t)b * p.H + h) * p.nq + i0);
+      }
+      if (left <= 0) qs.rows = ys.rows = 0;
       const uint32_t to = lds + slot * kDkvTilesStage;
-      ex_load_tile64(Qb, qpitch, i0, limit, ql, to, wave);
-      ex_load_tile64(Yb, ypitch, i0, limit, yl, to + kTile64, wave);
       if (wave < 2) {  // a plane of statistics each
-        const char* stat = reinterpret_cast<const char*>(p.rowstat + ((int64_t)wave * p.B * p.H + (int64_t)b * p.H + h) * p.nq);
-        u32x4_t rs = ex_rsrc(stat, 4, i0, 0, 4);
-        rs[2] = (uint32_t)__builtin_amdgcn_readfirstlane(max(min(limit - i0, 64), 0) * 4);
+        const uint64_t a = (uint64_t)(uintptr_t)stat;
+        u32x4_t rs;
+        rs[0] = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+        rs[1] = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu));
+        rs[2] = (uint32_t)__builtin_amdgcn_readfirstlane(max(min(qs.rows, 64), 0) * 4);
+        rs[3] = 0x00020000u;
         ex_load_lds4(rs, lane * 4, to + 2 * kTile64 + 256 * wave);
       }
+      ex_load_next64(qs, qpitch, ql, to, wave);
+      ex_load_next64(ys, ypitch, yl, to + kTile64, wave);
+      stat += 256;
       --left;
-      if (++lt == tiles.n) {
+      ++lt;
+      jump = lt == tiles.n || (tiles.first >= 0 && lt == 1);
+      if (lt == tiles.n) {
         lt = 0;
         ++lg;
       }
@@ -841,7 +863,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
 }
 
 // Adds up what k_exact_dkv leaves in parts: the first `sums` blocks the bias gradient, one (bucket, head)
-// per wave; the others dK and dV, eight columns of a key per thread.
+// per wave; the others dK and dV, four columns of a key per thread.
 template <typename T>
 __global__ __launch_bounds__(kExThreads) void k_exact_join_grads(ExactParams p, int sums) {
   const int lane = threadIdx.x & 63;
@@ -857,7 +879,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_join_grads(ExactParams p, 
     else static_cast<T*>(p.dtable)[e] = sum;
     return;
   }
-  const int64_t all = (int64_t)p.B * p.nk * p.Hk * kDHead, e = ((int64_t)(blockIdx.x - sums) * kExThreads + threadIdx.x) * 8;
+  const int64_t all = (int64_t)p.B * p.nk * p.Hk * kDHead, e = ((int64_t)(blockIdx.x - sums) * kExThreads + threadIdx.x) * 4;
   if (e >= all) return;
   const int col = (int)(e % (p.Hk * kDHead));
   const int64_t row = e / (p.Hk * kDHead);
@@ -866,78 +888,98 @@ __global__ __launch_bounds__(kExThreads) void k_exact_join_grads(ExactParams p, 
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     const float* from = (which ? p.part_dv : p.part_dk) + e;
-    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < p.kv_splits; ++s) {
-      const float4 x = *reinterpret_cast<const float4*>(from + s * all), y = *reinterpret_cast<const float4*>(from + s * all + 4);
-      o[0] += x.x, o[1] += x.y, o[2] += x.z, o[3] += x.w, o[4] += y.x, o[5] += y.y, o[6] += y.z, o[7] += y.w;
-    }
-    const float scale = live ? (which ? 1.f : p.scale) : 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) o[k] = live ? o[k] * scale : 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (live)
+      for (int s = 0; s < p.kv_splits; ++s) {
+        const float4 x = *reinterpret_cast<const float4*>(from + s * all);
+        o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
+      }
+    const float scale = which ? 1.f : p.scale;
     const ExactOut& t = which ? p.dV : p.dK;
-    ex_store8(static_cast<T*>(t.data) + b * t.batch + j * t.row + col, o);
+    ex_store4(static_cast<T*>(t.data) + b * t.batch + j * t.row + col,
+              make_float4(o.x * scale, o.y * scale, o.z * scale, o.w * scale));
   }
 }
+
+constexpr size_t kMaxLds = 163840;  // of a block: a CU's
 
 template <typename K>
 hipError_t set_lds(K kernel, size_t lds) {
+  if (lds > kMaxLds) return hipErrorInvalidValue;
   return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
 }
 
-// bf16 in blocks of 128 rows where the blocks of 32 are more than the CUs, which hold one of them each
-// (backward pass, 8 x 128 tokens, 12 heads: 20.3 against 13.9 us; 4 x 128, one round, 11.7 against 13.6;
-// 1 x 512 16.2 and 25.0, 2 x 512 34.6 and 25.6).
-bool dq_in_tiles(const ExactParams& p) { return p.bf16 && exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B > device_cus(); }
+// bf16 in blocks of 128 rows where the blocks of 32 are more than the CUs, or, in a long loop, which is all a
+// block of 128 has on a CU then, twice as many (backward pass, 12 heads: 8 x 128 tokens, 384 blocks of 32,
+// 16.7 against 14.8 us; 4 x 256 22.4 and 18.6; 2 x 512 26.1 and 31.9; 1 x 1024 34.4 and 44.1; 2 x 256, 192
+// blocks, 13.5 and 18.2).
+bool in_tiles(const ExactParams& p, int64_t blocks, int loop) {
+  return p.bf16 && blocks > (loop > 384 ? 2 : 1) * (int64_t)device_cus();
+}
+bool dq_in_tiles(const ExactParams& p) { return in_tiles(p, exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B, p.nk); }
+// And where a block of 32 keys would have a long way over the queries of its heads (64 tiles), which blocks of
+// 128 keys then share (exact_kv_splits): 2 x 1024 tokens, 16 heads on 2, 66 against 61 us; 1 x 8192, 1 head,
+// 130 and 107; 1 x 2048, 4 heads, 41 against 47.
 bool dkv_in_tiles(const ExactParams& p) {
-  const char* v = getenv("EXV");
-  if (v && atoi(v) == 3 && p.bf16) return p.G * ((p.nq + 31) / 32) > 32 || (int64_t)((p.nk + 31) / 32) * p.Hk * p.B > device_cus();
-  return p.bf16 && (int64_t)((p.nk + 31) / 32) * p.Hk * p.B > device_cus();
+  return in_tiles(p, (int64_t)((p.nk + 31) / 32) * p.Hk * p.B, p.G * p.nq) || (p.bf16 && (int64_t)p.G * ((p.nq + 31) / 32) > 64);
 }
 
+// The largest table (and a wave's sums along diagonals, as long) fits beside the tiles.
+constexpr size_t kMaxTable = (2 * kMaxBiasDistance + 129) * 4;
+static_assert(kDkvLds<float> + (kExWaves + 1) * kMaxTable <= kMaxLds && kDkvLds<uint16_t> + (kExWaves + 1) * kMaxTable <= kMaxLds &&
+              kDkvTilesLds + (kExWaves + 1) * kMaxTable <= kMaxLds / 2, "LDS of a block");
+
 template <typename T, bool BIAS>
-hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
-  const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
-  hipError_t e;
-  if constexpr (ExFmt<T>::ES == 2) {
-    if (dq_in_tiles(p)) {
-      const size_t lds = 6 * kTile64 + table;
-      if ((e = set_lds(k_exact_dq_tiles<BIAS>, lds)) != hipSuccess) return e;
-      const int64_t blocks = (int64_t)((p.nq + 127) / 128) * p.H * p.B;
-      hipLaunchKernelGGL((k_exact_dq_tiles<BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
-      return hipGetLastError();
-    }
-  }
-  const size_t lds = kDqLds<T> + table * p.Gp;
-  if ((e = set_lds(k_exact_dq<T, BIAS>, lds)) != hipSuccess) return e;
+hipError_t launch_dq_rows(const ExactParams& p, hipStream_t s) {
+  const size_t lds = kDqLds<T> + (BIAS ? (size_t)exact_bias_entries(p.D) * 4 * p.Gp : 0);
+  const hipError_t e = set_lds(k_exact_dq<T, BIAS>, lds);
+  if (e != hipSuccess) return e;
   const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
   hipLaunchKernelGGL((k_exact_dq<T, BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
   return hipGetLastError();
 }
 
 template <typename T, bool BIAS>
-hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
-  const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
-  const bool in_tiles = dkv_in_tiles(p);
-  // a block's share of the LDS (two blocks to a CU in tiles), its tiles, its waves' sums along diagonals
-  const size_t room = in_tiles ? 81920 : 163840, base = (in_tiles ? kDkvTilesLds : kDkvLds<T>) + 2 * kExWaves * table;
-  const int at_once = BIAS ? (int)((room - base) / table) : p.G;  // heads whose bias tables fit
-  const int heads = at_once < p.G ? at_once : p.G;
-  const size_t lds = base + table * heads;
-  const int64_t blocks = (int64_t)((p.nk + (in_tiles ? 127 : 31)) / (in_tiles ? 128 : 32)) * p.Hk * p.B * p.kv_splits;
-  hipError_t e;
+hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
   if constexpr (ExFmt<T>::ES == 2) {
-    if (in_tiles) {
-      if ((e = set_lds(k_exact_dkv_tiles<BIAS>, lds)) != hipSuccess) return e;
-      hipLaunchKernelGGL((k_exact_dkv_tiles<BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
+    if (dq_in_tiles(p)) {
+      const size_t lds = 6 * kTile64 + (BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0);
+      const hipError_t e = set_lds(k_exact_dq_tiles<BIAS>, lds);
+      if (e != hipSuccess) return e;
+      const int64_t blocks = (int64_t)((p.nq + 127) / 128) * p.H * p.B;
+      hipLaunchKernelGGL((k_exact_dq_tiles<BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
+      return hipGetLastError();
     }
   }
-  if (!in_tiles) {
-    if ((e = set_lds(k_exact_dkv<T, BIAS>, lds)) != hipSuccess) return e;
-    hipLaunchKernelGGL((k_exact_dkv<T, BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
+  return launch_dq_rows<T, BIAS>(p, s);
+}
+
+// A block's tiles and its waves' sums along diagonals in LDS, then the bias tables of as many heads as fit.
+template <bool BIAS, typename K>
+hipError_t launch_dkv_kernel(K kernel, const ExactParams& p, int keys, size_t base, hipStream_t s) {
+  const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
+  base += kExWaves * table;
+  int heads = p.G;
+  if constexpr (BIAS) {
+    const size_t room = base + table <= kMaxLds / 2 ? kMaxLds / 2 : kMaxLds;  // two blocks to a CU, or one
+    heads = (int)std::min<size_t>(heads, (room - base) / table);
   }
-  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const size_t lds = base + table * heads;
+  const hipError_t e = set_lds(kernel, lds);
+  if (e != hipSuccess) return e;
+  const int64_t blocks = (int64_t)((p.nk + keys - 1) / keys) * p.Hk * p.B * p.kv_splits;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
+  return hipGetLastError();
+}
+
+template <typename T, bool BIAS>
+hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
+  hipError_t e = hipErrorInvalidValue;
+  if (!dkv_in_tiles(p)) e = launch_dkv_kernel<BIAS>(k_exact_dkv<T, BIAS>, p, 32, kDkvLds<T>, s);
+  else if constexpr (ExFmt<T>::ES == 2) e = launch_dkv_kernel<BIAS>(k_exact_dkv_tiles<BIAS>, p, 128, kDkvTilesLds, s);
+  if (e != hipSuccess) return e;
   const int sums = BIAS ? (p.buckets * p.H + kExWaves - 1) / kExWaves : 0;
-  const int64_t rows = p.kv_splits > 1 ? ((int64_t)p.B * p.nk * p.Hk * (kDHead / 8) + kExThreads - 1) / kExThreads : 0;
+  const int64_t rows = p.kv_splits > 1 ? ((int64_t)p.B * p.nk * p.Hk * (kDHead / 4) + kExThreads - 1) / kExThreads : 0;
   if (sums + rows == 0) return hipSuccess;
   hipLaunchKernelGGL((k_exact_join_grads<T>), dim3((unsigned)(sums + rows)), dim3(kExThreads), 0, s, p, sums);
   return hipGetLastError();
@@ -952,14 +994,14 @@ hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
 }  // namespace
 
 // Blocks that share a key's queries: where they leave CUs without one (few keys, or few key heads with
-// many query heads), as many as that takes, of at least two tiles to a wave.
+// many query heads), as many as that takes, of sixteen tiles of 64 at least, or a tile of 32 to a wave
+// where that saves more than the join takes.
 int exact_kv_splits(const ExactParams& p) {
-  const bool in_tiles = dkv_in_tiles(p);
-  const int64_t blocks = (int64_t)((p.nk + (in_tiles ? 127 : 31)) / (in_tiles ? 128 : 32)) * p.Hk * p.B;
-  const int64_t tiles = (int64_t)p.G * ((p.nq + (in_tiles ? 63 : 31)) / (in_tiles ? 64 : 32));
-  const int64_t want = (in_tiles ? 2 : 1) * device_cus() / blocks, most = tiles / (in_tiles ? 4 : 2 * kExWaves);
-  const int64_t n = want < most ? want : most;
-  return n < 1 ? 1 : (int)n;
+  const bool big = dkv_in_tiles(p);
+  const int64_t blocks = (int64_t)((p.nk + (big ? 127 : 31)) / (big ? 128 : 32)) * p.Hk * p.B;
+  const int64_t tiles = (int64_t)p.G * ((p.nq + (big ? 63 : 31)) / (big ? 64 : 32));
+  const int64_t n = std::min((big ? 2 : 1) * device_cus() / blocks, tiles / (big ? 16 : kExWaves));
+  return n > 1 && (big || exact_worth(tiles, n, p.bf16 ? 2 : 8)) ? (int)n : 1;
 }
 
 int64_t exact_bias_parts(const ExactParams& p) {  // a part per wave of k_exact_dkv

@@ -5,6 +5,7 @@
 // y' = y 2^(m - m') + P V; Y = y / l and the log-sum-exp ln 2 (m + log2 l) at the end. The scores come
 // as S^T = K Q^T, so that a lane holds one query's scores: m, l and the rescaling are per lane, and
 // P feeds Y^T = V^T P^T from the registers it is in.
+#include <algorithm>
 #include "exact_device.h"
 #include "mca_kernels.h"
 
@@ -48,7 +49,7 @@ __device__ __forceinline__ void ex_softmax_step(ExState& s, f32x16_t& x) {
 // once for them. The key tiles are dealt out to the block's four waves and to `splits` blocks; a
 // wave loads its own tiles straight into LDS ahead of their use and waits for nobody until the
 // end, where the waves' states (and the blocks', in k_exact_join) are joined in a fixed order.
-template <typename T> constexpr int kRowStages = ExFmt<T>::ES == 2 ? 3 : 2;
+template <typename T> constexpr int kRowStages = ExFmt<T>::ES == 2 ? 2 : 1;
 template <typename T> constexpr int kRowLds = kExWaves * kRowStages<T> * 2 * tile_bytes<T>();
 
 template <typename T, bool BIAS>
@@ -149,67 +150,66 @@ __global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
           make_float4(s.y[cc][r], s.y[cc][r + 1], s.y[cc][r + 2], s.y[cc][r + 3]);
   if (hf == 0) ml[wave * 32 + c] = make_float2(s.m, s.l);
   __syncthreads();
-  // thread: row tid / 8, columns 8 (tid % 8) .. + 7
-  const int row = threadIdx.x >> 3, col = (threadIdx.x & 7) * 8;
-  float M = -INFINITY, L = 0.f, w[kExWaves], y[8];
+  // thread: 4 columns of two rows
 #pragma unroll
-  for (int k = 0; k < kExWaves; ++k) M = fmaxf(M, ml[k * 32 + row].x);
-  const float ref = M == -INFINITY ? 0.f : M;
+  for (int half = 0; half < 2; ++half) {
+    const int row = (threadIdx.x >> 4) + half * 16, col = (threadIdx.x & 15) * 4;
+    float M = -INFINITY, L = 0.f;
 #pragma unroll
-  for (int k = 0; k < kExWaves; ++k) {
-    w[k] = ex_exp2(ml[k * 32 + row].x - ref);
-    L += ml[k * 32 + row].y * w[k];
-  }
+    for (int k = 0; k < kExWaves; ++k) M = fmaxf(M, ml[k * 32 + row].x);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    y[e] = 0.f;
-#pragma unroll
-    for (int k = 0; k < kExWaves; ++k) y[e] += ys[(k * 32 + row) * YS + col + e] * w[k];
+    for (int k = 0; k < kExWaves; ++k) {
+      const float w = ex_exp2(ml[k * 32 + row].x - ref);
+      L += ml[k * 32 + row].y * w;
+      const float4 t = *reinterpret_cast<const float4*>(ys + (k * 32 + row) * YS + col);
+      y.x += t.x * w, y.y += t.y * w, y.z += t.z * w, y.w += t.w * w;
+    }
+    const int vr = vt * 32 + row, ir = vr / p.Gp, hr = hx * p.Gp + vr % p.Gp;
+    if (ir >= br.qlen) L = 0.f;  // a padded query
+    if (ir >= p.nq) continue;
+    if (p.splits > 1) {
+      const int64_t R = ((int64_t)(split * p.B + b) * Hx + hx) * nvt * 32 + vr;
+      *reinterpret_cast<float4*>(p.part_y + R * kDHead + col) = y;
+      if ((threadIdx.x & 15) == 0) p.part_ml[R] = make_float2(M, L);
+    } else {
+      const float inv = L > 0.f ? 1.f / L : 0.f;  // a row without keys is 0
+      T* o = static_cast<T*>(p.Yo.data) + b * p.Yo.batch + ir * p.Yo.row + hr * kDHead + col;
+      if (L == 0.f) y = make_float4(0.f, 0.f, 0.f, 0.f);
+      if constexpr (ES == 2) *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
+      else *reinterpret_cast<float4*>(o) = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+      if ((threadIdx.x & 15) == 0)
+        p.lse[((int64_t)b * p.H + hr) * p.nq + ir] = L > 0.f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
+    }
   }
-  const int vr = vt * 32 + row, ir = vr / p.Gp, hr = hx * p.Gp + vr % p.Gp;
-  if (ir >= br.qlen) L = 0.f;  // a padded query
-  if (p.splits > 1) {
-    const int64_t R = ((int64_t)(split * p.B + b) * Hx + hx) * nvt * 32 + vr;
-    float4* o = reinterpret_cast<float4*>(p.part_y + R * kDHead + col);
-    o[0] = make_float4(y[0], y[1], y[2], y[3]);
-    o[1] = make_float4(y[4], y[5], y[6], y[7]);
-    if ((threadIdx.x & 7) == 0) p.part_ml[R] = make_float2(M, L);
-    return;
-  }
-  if (ir >= p.nq) return;
-  const float inv = L > 0.f ? 1.f / L : 0.f;  // a row without keys is 0
-  T* o = static_cast<T*>(p.Yo.data) + b * p.Yo.batch + ir * p.Yo.row + hr * kDHead + col;
-  if constexpr (ES == 2) {
-    *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv),
-                                              pack_bf16x2(y[4] * inv, y[5] * inv), pack_bf16x2(y[6] * inv, y[7] * inv));
-  } else {
-    reinterpret_cast<float4*>(o)[0] = make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-    reinterpret_cast<float4*>(o)[1] = make_float4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv);
-  }
-  if ((threadIdx.x & 7) == 0)
-    p.lse[((int64_t)b * p.H + hr) * p.nq + ir] = L > 0.f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
 }
 
-// Joins the parts of a row: a wave per (query, head) row, a lane per column.
+// Joins the parts (at most 64) of a (query, head) row: a wave per row, a lane per part for the weights and per
+// column for the sums.
 template <typename T>
 __global__ __launch_bounds__(kExThreads) void k_exact_join(ExactParams p) {
-  const int lane = threadIdx.x & 63;
-  const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp;
-  const int64_t R = (int64_t)blockIdx.x * kExWaves + (threadIdx.x >> 6), rows = (int64_t)p.B * Hx * nvt * 32;
-  const int vr = (int)(R % (nvt * 32)), i = vr / p.Gp;
-  const int64_t bh = R / (nvt * 32);
-  if (R >= rows || i >= p.nq) return;
-  const int b = (int)(bh / Hx), h = (int)(bh % Hx) * p.Gp + vr % p.Gp;
-  float M = -INFINITY, L = 0.f, y = 0.f;
-  for (int s = 0; s < p.splits; ++s) M = fmaxf(M, p.part_ml[s * rows + R].x);
-  const float ref = M == -INFINITY ? 0.f : M;
-  for (int s = 0; s < p.splits; ++s) {
-    const float2 ml = p.part_ml[s * rows + R];
-    const float w = ex_exp2(ml.x - ref);
-    L += ml.y * w;
-    y += p.part_y[(s * rows + R) * kDHead + lane] * w;
+  const int lane = threadIdx.x & 63, nv = p.nq * p.Gp, nvt = (nv + 31) / 32, Hx = p.H / p.Gp;
+  const int64_t e = (int64_t)blockIdx.x * kExWaves + (threadIdx.x >> 6), rows = (int64_t)p.B * Hx * nvt * 32;
+  if (e >= (int64_t)p.B * Hx * nv) return;
+  const int v = (int)(e % nv), i = v / p.Gp;
+  const int64_t bh = e / nv, R = bh * nvt * 32 + v;
+  const int b = (int)(bh / Hx), h = (int)(bh % Hx) * p.Gp + v % p.Gp;
+  const float2 ml = lane < p.splits ? p.part_ml[lane * rows + R] : make_float2(-INFINITY, 0.f);
+  const float M = wave_max(ml.x), w = ex_exp2(ml.x - (M == -INFINITY ? 0.f : M));
+  float L = ml.y * w;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) L += __shfl_xor(L, o);
+  float y = 0.f;
+  for (int s0 = 0; s0 < p.splits; s0 += 8) {  // eight loads under way; parts past the last have weight 0
+    float t[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t[k] = p.part_y[(min(s0 + k, p.splits - 1) * rows + R) * kDHead + lane];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      y += t[k] * __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(w), s0 + k));
   }
-  y *= L > 0.f ? 1.f / L : 0.f;
+  y = L > 0.f ? y * (1.f / L) : 0.f;
   T* o = static_cast<T*>(p.Yo.data) + b * p.Yo.batch + i * p.Yo.row + h * kDHead + lane;
   if constexpr (ExFmt<T>::ES == 2) *o = (T)f32_to_bf16_bits(y);
   else *o = y;
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_join(ExactParams p) {
 // type's range. A row whose sum passes 2^64 (logits 44 above M), or whose first keys the bias all
 // masked and whose sum is below 2^-20, has its block take the pass again with a running maximum.
 template <bool BIAS, int MT>
-__global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT == 1 && !BIAS ? 3 : 2))) void k_exact_tiles(ExactParams p) {
+__global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 3 : 2))) void k_exact_tiles(ExactParams p) {
   constexpr int QB = 128 * MT;
   extern __shared__ __align__(16) char smem[];  // three K tiles, three V tiles, the bias table
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -242,8 +242,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
   const int qw = qt * QB + wave * 32 * MT;  // the wave's first query
   const int last = min(qt * QB + QB, br.qlen) - 1;
   const ExTiles tiles = last >= qt * QB ? ex_key_tiles<64>(p, br.pos + qt * QB, br.pos + last, br.klen) : ExTiles{-1, 0, 0};
-  // positions of the wave's queries that there are
-  const int wmin = br.pos + qw, wmax = br.pos + min(qw + 32 * MT, br.qlen) - 1;
+  // keys that all of the wave's queries attend
+  const ExRange whole = ex_whole_keys(p, br.pos + qw, br.pos + min(qw + 32 * MT, br.qlen) - 1, br.klen);
 
   char* yrow = static_cast<char*>(p.Yo.data) + ((int64_t)b * p.Yo.batch + (int64_t)qw * p.Yo.row + h * kDHead) * 2;
   float* lse = p.lse + ((int64_t)b * p.H + h) * p.nq;
@@ -252,12 +252,15 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
   const int kpitch = (int)p.K.row * 2, vpitch = (int)p.V.row * 2;
   const uint32_t kl = ex_load64(wave, lane, kpitch), vl = ex_load64<true>(wave, lane, vpitch);
   const uint32_t lds = lds_addr(smem);
-  auto load_k = [&](int t, int slot) __attribute__((always_inline)) {  // past the last tile: zeros
-    ex_load_tile64(Kb, kpitch, ex_tile_at(tiles, t) * 64, t < tiles.n ? br.klen : 0, kl, lds + slot * kTile64, wave);
+  // Tile t into buffer `slot`, in the order of t; past the last tile: zeros
+  ExStream ks, vs;
+  auto load = [&](ExStream& m, const char* base, int pitch, int t, uint32_t off, uint32_t to) __attribute__((always_inline)) {
+    if (t == 0 || (tiles.first >= 0 && t == 1)) m = ex_stream(base, pitch, ex_tile_at(tiles, t) * 64, br.klen);
+    if (t >= tiles.n) m.rows = 0;
+    ex_load_next64(m, pitch, off, to, wave);
   };
-  auto load_v = [&](int t, int slot) __attribute__((always_inline)) {
-    ex_load_tile64(Vb, vpitch, ex_tile_at(tiles, t) * 64, t < tiles.n ? br.klen : 0, vl, lds + (3 + slot) * kTile64, wave);
-  };
+  auto load_k = [&](int t, int slot) __attribute__((always_inline)) { load(ks, Kb, kpitch, t, kl, lds + slot * kTile64); };
+  auto load_v = [&](int t, int slot) __attribute__((always_inline)) { load(vs, Vb, vpitch, t, vl, lds + (3 + slot) * kTile64); };
   load_k(0, 0);
   ExRow<uint16_t> q[MT];
 #pragma unroll
@@ -316,11 +319,11 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
         }
       }
     }
-    if (__builtin_expect(!ex_whole(p, wmin, wmax, k0, br.klen), 0)) {
+    if (__builtin_expect(!ex_has(whole, k0), 0)) {
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         const ExSpan keys = ex_keys_of(p, br.pos + qw + 32 * m + ex_opaque(c), br.klen);
-        ex_mask(s[m], keys, k0 + 4 * hf, k0 > 0);
+        ex_mask(s[m], keys, k0 + 4 * hf, MT == 2 || k0 > 0);  // 256 queries: no window
       }
     }
   };
@@ -429,7 +432,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
       s.l = 0.f;
       s.y[0] = s.y[1] = zero;
       const int first = qw + 32 * m, ln = ex_opaque(lane), cs = ln & 31, hs = ln >> 5, pos = br.pos + first + cs;
-      const ExCols64<true> vs = ex_cols64<true>(ln);
+      const ExCols64<true> vc = ex_cols64<true>(ln);
       const ExSpan keys = ex_keys_of(p, pos, br.klen);
       const char* row = static_cast<const char*>(p.Q.data) +
                         ((int64_t)b * p.Q.batch + (int64_t)min(first + cs, br.qlen - 1) * p.Q.row + h * kDHead) * 2;
@@ -459,7 +462,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
             for (int w = 0; w < 4; ++w) x8[w] = pack_bf16x2(x[8 * pp + 2 * w], x[8 * pp + 2 * w + 1]);
 #pragma unroll
             for (int cc = 0; cc < 2; ++cc)
-              s.y[cc] = ex_mfma<uint16_t>(ex_read_col(smem + 3 * kTile64, vs, half, pp, cc), x8, s.y[cc]);
+              s.y[cc] = ex_mfma<uint16_t>(ex_read_col(smem + 3 * kTile64, vc, half, pp, cc), x8, s.y[cc]);
           }
         }
         __syncthreads();
@@ -490,7 +493,7 @@ hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
   const int64_t rows = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
   hipLaunchKernelGGL((k_exact_rows<T, BIAS>), dim3((unsigned)(rows * p.splits)), dim3(kExThreads), lds, s, p);
   if ((e = hipGetLastError()) != hipSuccess || p.splits == 1) return e;
-  hipLaunchKernelGGL((k_exact_join<T>), dim3((unsigned)(rows * 32 / kExWaves)), dim3(kExThreads), 0, s, p);
+  hipLaunchKernelGGL((k_exact_join<T>), dim3((unsigned)(((int64_t)p.B * p.H * p.nq + kExWaves - 1) / kExWaves)), dim3(kExThreads), 0, s, p);
   return hipGetLastError();
 }
 
@@ -499,14 +502,13 @@ hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
 // Heads side by side in the kernels of 32 rows: a key head's whole group, unless its bias tables do not
 // fit beside the tiles.
 int exact_group(const ExactParams& p) {
-  return !p.table || (int64_t)p.G * exact_bias_entries(p.D) <= 8192 ? p.G : 1;
+  return !p.table || (int64_t)p.G * exact_bias_entries(p.D) * 4 <= 163840 - kRowLds<float> ? p.G : 1;
 }
 
-// bf16 in blocks of 128 queries or more: where the blocks of 32 rows are more than the CUs (one of those
-// fills a CU's LDS, so a second round of them doubles the time: 8 x 128 tokens, 12 heads 8.8 against
-// 6.2 us; 4 x 128, one round, 5.3 against 6.1; 2 x 512 14.2 and 10.9, 1 x 512 7.4 and 10.7). Rows of a
-// single block of 32 over many keys stay: its four waves share the keys, of which a wave of the
-// other kernel reads all.
+// bf16 in blocks of 128 queries or more: where the blocks of 32 rows are more than the CUs (forward, 12
+// heads: 8 x 128 tokens, 384 blocks of 32, 6.9 against 6.3 us; 16 x 64 6.6 and 5.4; 1 x 1024 23.8 and 16.6;
+// 2 x 256, 192 blocks, 6.1 and 7.8; 1 x 512 7.5 and 10.5). Rows of a single block of 32 over many keys
+// stay: its four waves share the keys, of which a wave of the other kernel reads all.
 static bool forward_in_tiles(const ExactParams& p) {
   return p.bf16 && exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B > device_cus() &&
          (p.nq * p.Gp > 32 || p.nk <= 512);
@@ -522,13 +524,19 @@ static bool forward_wide(const ExactParams& p) {
   return !p.table && !p.window && 4 * blocks_per_cu(q128 * pairs) > 7 * blocks_per_cu((q128 + 1) / 2 * pairs);
 }
 
-// Blocks that share a row's keys: as many as fill the card four times over, where every wave still
-// gets four tiles.
+// Blocks that share a row's keys. Enough to give every CU one, of three tiles to a wave at least (float32,
+// whose tiles take four times as long: less than one); or, where the keys are so long that sixteen tiles
+// stay to a wave (four), up to four to a CU, which even out rows of different lengths. Not for less than
+// the join takes. A token, 12 heads, bf16: 1500 keys 12.3 us in one part, 9.7 in 4, 10.2 in 8; 4000 keys
+// 25.5, 13.0, 11.5; 16000 keys 111, 20.5 in 16; 701 keys 8.3, 9.0 in 4. 32 tokens, 16 heads on 4, 2048 to
+// 16384 keys: 86.5 us in 2 parts, 66.9 in 8, 80.3 in 32.
 int exact_splits(const ExactParams& p) {
   if (forward_in_tiles(p)) return 1;
   const int64_t rows = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B, tiles = (p.nk + 31) / 32;
-  const int64_t want = (4 * device_cus() + rows - 1) / rows, most = tiles / (4 * kExWaves);
-  return (int)(want < most ? (want < 1 ? 1 : want) : (most < 1 ? 1 : most));
+  const int64_t fill = std::min((device_cus() + rows - 1) / rows, tiles / (p.bf16 ? 12 : 3));
+  const int64_t even = std::min(4 * device_cus() / rows, tiles / (p.bf16 ? 64 : 16));
+  const int64_t n = std::min<int64_t>(std::max<int64_t>(std::max(fill, even), 1), 64);
+  return exact_worth(tiles, n, p.bf16 ? 1 : 4) ? (int)n : 1;
 }
 
 hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s) {
