@@ -140,13 +140,36 @@ __device__ __forceinline__ float ex_sum16(const T& x) {
   return s;
 }
 
+// D plus the lane's part of a . b.
+template <typename T>
+__device__ __forceinline__ float ex_row_dot(const ExRow<T>& a, const ExRow<T>& b, float D) {
+#pragma unroll
+  for (int k = 0; k < ExFmt<T>::NG; ++k)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if constexpr (ExFmt<T>::ES == 2) {
+        D = fmaf(__uint_as_float(a.v[k][w] << 16), __uint_as_float(b.v[k][w] << 16), D);
+        D = fmaf(__uint_as_float(a.v[k][w] & 0xffff0000u), __uint_as_float(b.v[k][w] & 0xffff0000u), D);
+      } else {
+        D = fmaf(__uint_as_float(a.v[k][w]), __uint_as_float(b.v[k][w]), D);
+      }
+    }
+  return D;
+}
+
 // ------------------------------------------------------------------ dQ
 // Blocks of 32 (query, head) rows whose key tiles the waves share, as k_exact_rows. S^T = K Q^T
 // and dP^T = V dY^T: the row's c and D are one value per lane, and dS feeds dQ^T = K^T dS^T.
 //
 //
-// With a bias in bfloat16, D = dY . Y of the rounded Y is not what the bias gradient asks for, whose sums
-// cancel: sum_j dS_ij, which is 0 for the exact D, is added to the D that k_exact_dkv takes.
+// dS cancels where attention is sharp, and in bf16 D' = dY . Y of the rounded Y (whose P were rounded too)
+// is not exact enough then: the gradients would lose as much as by all other roundings (8 x 300 tokens,
+// logits of standard deviation 2: dQ off by 3.8e-3 of its norm; 2.4e-3 with the exact D, 1.7e-3 of it the
+// result's own rounding). The exact D comes out of the sums: sum_j dS'_ij = D - D', so sum_j P_ij k_j is
+// summed beside dq, dq = scale (sum_j dS' k - (D - D') sum_j P k), and k_exact_dkv gets D. What D - D' is
+// comes from large P, and is multiplied by them: the kernel of 64-row tiles leaves half tiles out of sum_j P k
+// whose P are all at most kSmallP (at 4 x 4096 tokens, 12 heads, all of them: dQ 317 us without this, 427
+// with every tile's product).
 template <typename T, bool BIAS>
 __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
   extern __shared__ __align__(16) char smem[];
@@ -189,18 +212,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
   const ExRow<T> dy = live ? ex_global_row<T>(dyrow, hf) : ex_zero_row<T>();
   float D = 0.f, cr = INFINITY;  // a row without keys, or behind the last query: every P is 0
   if (live) {
-    const ExRow<T> y = ex_global_row<T>(yrow, hf);
-#pragma unroll
-    for (int k = 0; k < ExFmt<T>::NG; ++k)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        if constexpr (ES == 2) {
-          D = fmaf(__uint_as_float(y.v[k][w] << 16), __uint_as_float(dy.v[k][w] << 16), D);
-          D = fmaf(__uint_as_float(y.v[k][w] & 0xffff0000u), __uint_as_float(dy.v[k][w] & 0xffff0000u), D);
-        } else {
-          D = fmaf(__uint_as_float(y.v[k][w]), __uint_as_float(dy.v[k][w]), D);
-        }
-      }
+    D = ex_row_dot<T>(dy, ex_global_row<T>(yrow, hf), D);
     const float lse = p.lse[((int64_t)b * p.H + head) * p.nq + i];
     cr = lse == -INFINITY ? INFINITY : lse * kLog2e;
   }
@@ -214,7 +226,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
     __syncthreads();
     tl = tb + g * n + p.D + 64;
   }
-  f32x16_t dq[2] = {ex_zero16(), ex_zero16()};
+  f32x16_t dq[2] = {ex_zero16(), ex_zero16()}, pk[2] = {ex_zero16(), ex_zero16()};
 
   int slot = 0;
   for (int idx = wave; idx < tiles.n; idx += kExWaves) {
@@ -246,26 +258,34 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
       ex_mask(x, keys, k0 + 4 * hf, k0 > 0);
     }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = ex_exp2(x[r]) * (dp[r] - D);
+    for (int r = 0; r < 16; ++r) x[r] = ex_exp2(x[r]);
+    if constexpr (ES == 2) ex_cols_product<T>(pk, kt, x, lane);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] *= dp[r] - D;
     ex_cols_product<T>(dq, kt, x, lane);
-    if constexpr (BIAS && ES == 2) rest += ex_sum16(x);
+    if constexpr (ES == 2) rest += ex_sum16(x);
     slot = slot == ST - 1 ? 0 : slot + 1;
   }
   wait_vmcnt<0>();  // no load is under way into what is written next
   __syncthreads();
   float* ys = reinterpret_cast<float*>(smem);
-  ex_put_sums(ys, dq, wave * 32 + c, hf);
-  float* rests = ys + kExWaves * 32 * kYS;  // [wave][row]
-  if constexpr (BIAS && ES == 2) {
+  if constexpr (ES == 2) {
+    float* rests = ys + kExWaves * 32 * kYS;  // [wave][row]
     rest += ex_other_half(rest);
     if (hf == 0) rests[wave * 32 + c] = rest;
+    __syncthreads();
+    rest = 0.f;
+#pragma unroll
+    for (int k = 0; k < kExWaves; ++k) rest += rests[k * 32 + c];
+    D += rest;
+#pragma unroll
+    for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq[cc][r] = fmaf(-rest, pk[cc][r], dq[cc][r]);
   }
+  ex_put_sums(ys, dq, wave * 32 + c, hf);
+  if (wave == 0 && hf == 0 && i < p.nq) ex_put_stat<T>(p, ((int64_t)b * p.H + head) * p.nq + i, cr, D);
   __syncthreads();
-  if (wave == 0 && hf == 0 && i < p.nq) {
-    if constexpr (BIAS && ES == 2)
-      for (int k = 0; k < kExWaves; ++k) D += rests[k * 32 + c];
-    ex_put_stat<T>(p, ((int64_t)b * p.H + head) * p.nq + i, cr, D);
-  }
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     const int row = (threadIdx.x >> 4) + half * 16, col = (threadIdx.x & 15) * 4;
@@ -463,6 +483,8 @@ __device__ __forceinline__ ExPair ex_pair(const f32x16_t& s, int j, float fac, f
   return r;
 }
 
+constexpr float kSmallP = 0x1p-6f;
+
 template <bool BIAS>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_dq_tiles(ExactParams p) {
   extern __shared__ __align__(16) char smem[];  // three K tiles, three V tiles, the bias table
@@ -503,15 +525,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   if (live) {
     q = ex_global_row<uint16_t>(static_cast<const char*>(p.Q.data) + (b * p.Q.batch + i * p.Q.row + hcol) * 2, hf);
     dy = ex_global_row<uint16_t>(static_cast<const char*>(p.dY.data) + (b * p.dY.batch + i * p.dY.row + hcol) * 2, hf);
-    const ExRow<uint16_t> y =
-        ex_global_row<uint16_t>(static_cast<const char*>(p.Y.data) + (b * p.Y.batch + i * p.Y.row + hcol) * 2, hf);
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        D = fmaf(__uint_as_float(y.v[k][w] << 16), __uint_as_float(dy.v[k][w] << 16), D);
-        D = fmaf(__uint_as_float(y.v[k][w] & 0xffff0000u), __uint_as_float(dy.v[k][w] & 0xffff0000u), D);
-      }
+    D = ex_row_dot<uint16_t>(
+        dy, ex_global_row<uint16_t>(static_cast<const char*>(p.Y.data) + (b * p.Y.batch + i * p.Y.row + hcol) * 2, hf), D);
     const float lse = p.lse[((int64_t)b * p.H + h) * p.nq + i];
     cr = lse == -INFINITY ? INFINITY : lse * kLog2e;
   }
@@ -530,8 +545,9 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   const ExRows64 ra = ex_rows64(lane);
   const ExCols64<false> ca = ex_cols64<false>(lane);
   const f32x16_t zero = ex_zero16();
-  f32x16_t dq[2] = {zero, zero}, s0, s1, p0, p1;
+  f32x16_t dq[2] = {zero, zero}, pk[2] = {zero, zero}, s0, s1, p0, p1;
   u32x4_t fr[kAhead], ds[2];
+  f32x16_t pr;
   // Operand of slot j: K, V chunk j / 2 in turn of half tile (kt, half), then K columns of (ct, chalf).
   auto read = [&](int j, const char* kt, int half, const char* ct, int chalf) __attribute__((always_inline)) {
     if (j < 8) return ex_read_row(kt + (j & 1) * 3 * kTile64, ra, half, j >> 1);
@@ -562,6 +578,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   auto step = [&](f32x16_t& s, f32x16_t& d, f32x16_t& sn, f32x16_t& dn, const char* ct, int ch, const char* nt, int nh,
                   const char* ft, int fh) __attribute__((always_inline)) {
     ExPair e{0.f, 0.f};
+    float most = 0.f;
 #pragma unroll
     for (int j = 0; j < 12; ++j) {
       if (j < 8) {
@@ -579,13 +596,26 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
           const int k = j - 1;
           d[2 * k] *= b4.e0;
           d[2 * k + 1] *= b4.e1;
-          if constexpr (BIAS) rest += d[2 * k] + d[2 * k + 1];
+          rest += d[2 * k] + d[2 * k + 1];
+          pr[2 * k] = b4.e0;
+          pr[2 * k + 1] = b4.e1;
+          most = fmaxf(fmaxf(most, b4.e0), b4.e1);
           uint32_t w = pack_bf16x2(d[2 * k], d[2 * k + 1]);
           ex_pin(w);
           ds[k >> 2][k & 3] = w;
         }
       }
       __builtin_amdgcn_sched_barrier(0);
+    }
+    if (__builtin_expect(__any(most > kSmallP), 0)) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        u32x4_t w;
+#pragma unroll
+        for (int l = 0; l < 4; ++l) w[l] = pack_bf16x2(pr[8 * k + 2 * l], pr[8 * k + 2 * l + 1]);
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc) pk[cc] = ex_mfma<uint16_t>(ex_read_col(ct, ca, ch, k, cc), w, pk[cc]);
+      }
     }
   };
 
@@ -618,7 +648,12 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     b1 = b2;
     b2 = o;
   }
-  if constexpr (BIAS) D += rest + ex_other_half(rest);
+  rest += ex_other_half(rest);
+  D += rest;
+#pragma unroll
+  for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dq[cc][r] = fmaf(-rest, pk[cc][r], dq[cc][r]);
   if (hf == 0 && i < p.nq) ex_put_stat<uint16_t>(p, ((int64_t)b * p.H + h) * p.nq + i, cr, D);
   wait_vmcnt<0>();  // no load is under way into what is written next
   __syncthreads();
@@ -930,28 +965,23 @@ static_assert(kDkvLds<float> + (kExWaves + 1) * kMaxTable <= kMaxLds && kDkvLds<
               kDkvTilesLds + (kExWaves + 1) * kMaxTable <= kMaxLds / 2, "LDS of a block");
 
 template <typename T, bool BIAS>
-hipError_t launch_dq_rows(const ExactParams& p, hipStream_t s) {
-  const size_t lds = kDqLds<T> + (BIAS ? (size_t)exact_bias_entries(p.D) * 4 * p.Gp : 0);
-  const hipError_t e = set_lds(k_exact_dq<T, BIAS>, lds);
-  if (e != hipSuccess) return e;
-  const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
-  hipLaunchKernelGGL((k_exact_dq<T, BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
-  return hipGetLastError();
-}
-
-template <typename T, bool BIAS>
 hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
+  const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
+  hipError_t e;
   if constexpr (ExFmt<T>::ES == 2) {
     if (dq_in_tiles(p)) {
-      const size_t lds = 6 * kTile64 + (BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0);
-      const hipError_t e = set_lds(k_exact_dq_tiles<BIAS>, lds);
-      if (e != hipSuccess) return e;
+      const size_t lds = 6 * kTile64 + table;
+      if ((e = set_lds(k_exact_dq_tiles<BIAS>, lds)) != hipSuccess) return e;
       const int64_t blocks = (int64_t)((p.nq + 127) / 128) * p.H * p.B;
       hipLaunchKernelGGL((k_exact_dq_tiles<BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
       return hipGetLastError();
     }
   }
-  return launch_dq_rows<T, BIAS>(p, s);
+  const size_t lds = kDqLds<T> + table * p.Gp;
+  if ((e = set_lds(k_exact_dq<T, BIAS>, lds)) != hipSuccess) return e;
+  const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
+  hipLaunchKernelGGL((k_exact_dq<T, BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
+  return hipGetLastError();
 }
 
 // A block's tiles and its waves' sums along diagonals in LDS, then the bias tables of as many heads as fit.
