@@ -415,14 +415,14 @@ class ExactGradients:
     dbias: object = None
 
 
-def _exact_rows(name, t, shape, like) -> Rows:
-    if not t.is_cuda or t.device != like.device or t.dtype != like.dtype:
-        raise ValueError(f"{name} must be a {like.dtype} tensor on {like.device}")
-    if tuple(t.shape) != tuple(shape) or t.stride(2) != 1:
-        raise ValueError(f"{name} must be {list(shape)} with contiguous columns (got {list(t.shape)}, strides {t.stride()})")
+def _exact_rows(name, t, shape, dtype, device) -> Rows:
+    if t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be a {dtype} tensor on {device}")
+    stride = t.stride()
+    if t.shape != shape or stride[2] != 1:
+        raise ValueError(f"{name} must be {list(shape)} with contiguous columns (got {list(t.shape)}, strides {stride})")
     # a row or batch stride that nothing steps over may be anything
-    row = t.stride(1) if shape[1] > 1 else shape[2]
-    return Rows(t.data_ptr(), t.stride(0) if shape[0] > 1 else 0, row)
+    return Rows(t.data_ptr(), stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else shape[2])
 
 
 class _ExactCall:
@@ -435,35 +435,34 @@ class _ExactCall:
             raise ValueError("Q, K and V must be 3-D device tensors")
         kv_heads = heads if kv_heads is None else kv_heads
         (B, nq, _), nk = Q.shape, K.shape[1]
-        self.q_shape, self.k_shape, self.device = (B, nq, heads * 64), (B, nk, kv_heads * 64), Q.device
-        self.dtype, self.lse_shape = Q.dtype, (B, heads, nq)
-        self.q, self.k, self.v = (_exact_rows(n, t, s, Q) for n, t, s in
-                                  (("Q", Q, self.q_shape), ("K", K, self.k_shape), ("V", V, self.k_shape)))
+        dev, dtype = self.device, self.dtype = Q.device, Q.dtype
+        self.q_shape, self.k_shape, self.lse_shape = (B, nq, heads * 64), (B, nk, kv_heads * 64), (B, heads, nq)
+        self.q = _exact_rows("Q", Q, self.q_shape, dtype, dev)
+        self.k = _exact_rows("K", K, self.k_shape, dtype, dev)
+        self.v = _exact_rows("V", V, self.k_shape, dtype, dev)
+        lens = []
         for name, t in (("q_lens", q_lens), ("kv_lens", kv_lens), ("q_pos", q_pos)):
-            if t is not None and (t.dtype != torch.int32 or t.shape != (B,) or t.device != Q.device or not t.is_contiguous()):
-                raise ValueError(f"{name} must be contiguous int32 [{B}] on {Q.device}")
-        d = self.desc = ExactDesc()
-        d.batch, d.q_len, d.kv_len, d.heads, d.kv_heads, d.d_head = B, nq, nk, heads, kv_heads, 64
-        d.dtype, d.causal, d.window = _dtype_code(Q), int(bool(causal)), int(window)
-        d.scale = 0.125 if scale is None else float(scale)
-        d.q_lens, d.kv_lens, d.q_pos = _ptr(q_lens), _ptr(kv_lens), _ptr(q_pos)
+            if t is not None and (t.dtype != torch.int32 or t.shape != (B,) or t.device != dev or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous int32 [{B}] on {dev}")
+            lens.append(None if t is None else t.data_ptr())
+        d = self.desc = ExactDesc(B, nq, nk, heads, kv_heads, 64, _dtype_code(Q), int(bool(causal)), int(window),
+                                  0.125 if scale is None else float(scale), *lens)
         self.table = None
         if bias is not None:
             t = self.table = bias.table
-            if t.dim() != 2 or t.shape[1] != heads or t.dtype != Q.dtype or t.device != Q.device or not t.is_contiguous():
-                raise ValueError(f"bias.table must be a contiguous {Q.dtype} [buckets, {heads}] on {Q.device}")
+            if t.dim() != 2 or t.shape[1] != heads or t.dtype != dtype or t.device != dev or not t.is_contiguous():
+                raise ValueError(f"bias.table must be a contiguous {dtype} [buckets, {heads}] on {dev}")
             d.bias_table, d.bias_buckets = t.data_ptr(), t.shape[0]
             d.bias_max_distance, d.bias_bidirectional = int(bias.max_distance), int(bool(bias.bidirectional))
-        self.like = Q
         self._keep = (Q, K, V, q_lens, kv_lens, q_pos, bias)
 
     def rows(self, name, t, shape) -> Rows:
-        return _exact_rows(name, t, shape, self.like)
+        return _exact_rows(name, t, shape, self.dtype, self.device)
 
     def check_lse(self, lse):
         import torch
 
-        if lse.dtype != torch.float32 or tuple(lse.shape) != self.lse_shape or lse.device != self.device or not lse.is_contiguous():
+        if lse.dtype != torch.float32 or lse.shape != self.lse_shape or lse.device != self.device or not lse.is_contiguous():
             raise ValueError(f"lse must be contiguous float32 {list(self.lse_shape)} on {self.device}")
         return lse
 
@@ -484,10 +483,17 @@ class _ExactCall:
 
         return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
 
-    def on_device(self):
+    def run(self, fn, name, args):
+        """fn(*args, stream) on the current stream of the tensors' device, with that device current."""
         import torch
 
-        return torch.cuda.device(self.device)
+        if torch.cuda.current_device() == self.device.index:
+            st = fn(*args, torch.cuda.current_stream(self.device).cuda_stream)
+        else:
+            with torch.cuda.device(self.device):
+                st = fn(*args, torch.cuda.current_stream(self.device).cuda_stream)
+        if st != MCA_OK:
+            _check(st, name)
 
 
 def _bytes(t) -> int:
@@ -519,9 +525,8 @@ def exact_attention_forward(Q, K, V, *, heads: int, kv_heads: Optional[int] = No
     Y, lse = out if out is not None else (call.new(call.q_shape), call.new(call.lse_shape, torch.float32))
     y = call.rows("Y", Y, call.q_shape)
     call.check_lse(lse)
-    with call.on_device():
-        _check(lib.mca_exact_attention_forward(call.desc, call.q, call.k, call.v, y, _ptr(lse), _ptr(ws), _bytes(ws),
-                                               _stream_handle(call.device)), "mca_exact_attention_forward")
+    call.run(lib.mca_exact_attention_forward, "mca_exact_attention_forward",
+             (call.desc, call.q, call.k, call.v, y, _ptr(lse), _ptr(ws), _bytes(ws)))
     return ExactResult(Y, lse)
 
 
@@ -545,10 +550,8 @@ def exact_attention_backward(dY, Q, K, V, Y, lse, *, heads: int, kv_heads: Optio
     if (bias is None) != (dbias is None) or dbias is not None and (
             dbias.shape != bias.table.shape or dbias.dtype != Q.dtype or dbias.device != Q.device or not dbias.is_contiguous()):
         raise ValueError("dbias must have the bias table's shape, dtype and device (None without a bias)")
-    with call.on_device():
-        _check(lib.mca_exact_attention_backward(call.desc, dy, call.q, call.k, call.v, y, _ptr(lse), dq, dk, dv, _ptr(dbias),
-                                                _ptr(ws), _bytes(ws), _stream_handle(call.device)),
-               "mca_exact_attention_backward")
+    call.run(lib.mca_exact_attention_backward, "mca_exact_attention_backward",
+             (call.desc, dy, call.q, call.k, call.v, y, _ptr(lse), dq, dk, dv, _ptr(dbias), _ptr(ws), _bytes(ws)))
     return ExactGradients(dQ, dK, dV, dbias)
 
 
@@ -583,22 +586,11 @@ class ExactPlan:
             self._backward = (lib.mca_exact_attention_backward, "mca_exact_attention_backward",
                               tuple(ctypes.byref(x) for x in [c.desc] + rows) + (_ptr(self.lse),) +
                               tuple(ctypes.byref(x) for x in grads) + (_ptr(self.dbias), _ptr(wb), _bytes(wb)))
-        self._current_device, self._index = torch.cuda.current_device, c.device.index
-
-    def _run(self, bound):
-        fn, name, args = bound
-        if self._current_device() != self._index:
-            with self._call.on_device():
-                st = fn(*args, _stream_handle(self._call.device))
-        else:
-            st = fn(*args, _stream_handle(self._call.device))
-        if st != MCA_OK:
-            _check(st, name)
 
     def forward(self):
-        self._run(self._forward)
+        self._call.run(*self._forward)
 
     def backward(self):
         if self._backward is None:
             raise ValueError("the plan was made without dY")
-        self._run(self._backward)
+        self._call.run(*self._backward)

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <atomic>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -54,6 +55,22 @@ struct ExactParams {
 inline int exact_bias_entries(int D) { return 2 * D + 129; }  // rel = j - p in [-D - 64, D + 64]
 // Rows (query, head) that the kernels of 32 rows pad to.
 inline int64_t exact_row_tiles(int64_t nq, int64_t Gp) { return (nq * Gp + 31) / 32; }
+
+constexpr size_t kMaxLds = 163840;  // of a block: a CU's
+
+// Allows kernel K that much LDS, once per device; an error where `lds` is more.
+template <auto K>
+hipError_t exact_set_lds(size_t lds) {
+  static std::atomic<int> allowed[64];
+  int dev = 0;
+  if (lds > kMaxLds) return hipErrorInvalidValue;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+  if (allowed[dev].load(std::memory_order_acquire)) return hipSuccess;
+  // idempotent: threads racing here all set the same attribute before any of them launches
+  const hipError_t e = hipFuncSetAttribute((const void*)K, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxLds);
+  if (e == hipSuccess) allowed[dev].store(1, std::memory_order_release);
+  return e;
+}
 
 // Whether `tiles` of 32 over four waves are worth splitting into n parts: what that saves in tiles one after
 // another, each `unit` times 0.55 us, against the 3 us of the launch that joins them.

@@ -14,10 +14,10 @@
 namespace mca {
 namespace {
 
-template <typename T> constexpr int kBwdStages = ExFmt<T>::ES == 2 ? 2 : 1;
-template <typename T> constexpr int kDqLds = kExWaves * kBwdStages<T> * 2 * tile_bytes<T>();
+// ST: tiles in LDS per wave of the kernels of 32 rows, all but one of them on their way.
+template <typename T, int ST> constexpr int kDqLds = kExWaves * ST * 2 * tile_bytes<T>();
 template <typename T> constexpr int kDkvStage = 2 * tile_bytes<T>() + 512;  // Q, dY, two planes of statistics
-template <typename T> constexpr int kDkvLds = kExWaves * kBwdStages<T> * kDkvStage<T>;
+template <typename T, int ST> constexpr int kDkvLds = kExWaves * ST * kDkvStage<T>;
 constexpr int kYS = kDHead + 4;  // row pitch of the sums that the waves of a block join in LDS
 
 // Four consecutive values of a row to `o`.
@@ -58,9 +58,10 @@ __device__ __forceinline__ void ex_put_stat(const ExactParams& p, int64_t row, f
 // k_exact_dkv a lane is a key and a register a query, so a step to the next query and the next
 // key is a step to the next register and lane: sums of the form acc = shift(acc) + x[r], one vector
 // instruction per pair with the lane shift in it, collect diagonals. A shift stays within 16 lanes
-// and what it pushes out is lost: shifting up collects the diagonals rel <= 0 of a block of 16 keys and
-// 16 queries, shifting down those of rel > 0. (Adding every pair to an array with LDS atomics took 130
-// cycles an instruction: 16 x 512 tokens, 12 heads, 306 us for the kernel that had it.)
+// and what it pushes out is lost: of a block of 16 keys and 16 queries, shifting up collects the
+// diagonals rel < 0, one to a lane, shifting down those of rel >= 0. (Adding every pair to an array with
+// LDS atomics took 130 cycles an instruction: 16 x 512 tokens, 12 heads, 306 us for the kernel that had
+// it.)
 template <int CTRL>
 __device__ __forceinline__ float ex_shift(float v) {  // within rows of 16 lanes, zeros shifted in
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
@@ -70,37 +71,68 @@ __device__ __forceinline__ float ex_shift_rows(float v) {  // only the rows of 1
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), CTRL,
                                                                ROWS, 0xF, true));
 }
-// Adds a tile's sums to a wave's array: `at` is the entry of rel = key 0 - query 0.
-__device__ __forceinline__ void ex_diagonals(const f32x16_t& x, float* at, int lane_) {
+template <int ROWS>
+__device__ __forceinline__ float ex_rows_only(float v) {  // zeros in the other rows
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0xE4, ROWS, 0xF, false));
+}
+// A wave's sums: dg, an array of entries, and the lower half of the last tile's, in lanes 32 and up. A diagonal of a
+// wave's keys passes two tiles of queries, one after the other, so what the next tile has is added in a
+// register and every entry is stored once.
+struct ExDiag {
+  float* dg;
+  float pend;
+  int at;  // the entry of pend's lane 32, -1: none
+};
+__device__ __forceinline__ void ex_diag_flush(ExDiag& d, int lane) {
+  if (d.at >= 0 && lane >= 32) d.dg[d.at + lane - 32] = d.pend;
+  d.at = -1;
+}
+// Tile x, whose key 0 and query 0 have entry `at`: its diagonals are the entries at - 31 .. at + 31.
+__device__ __forceinline__ void ex_diagonals(ExDiag& d, const f32x16_t& x, int at, int lane_) {
   const int lane = ex_opaque(lane_);
-  const int a = (lane >> 4) & 1, f = lane & 15;
-  float* o = at + (lane < 32 ? f - 15 : f) + 16 * a;
+  float up[2], down[2];
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {  // queries 16 kb + {0 .. 3, 8 .. 11} + 4 hf
-    float up = x[8 * kb], down = x[8 * kb + 7];
-#pragma unroll
-    for (int r = 1; r < 8; ++r) {
-      up = (r == 4 ? ex_shift<0x115>(up) : ex_shift<0x111>(up)) + x[8 * kb + r];
-      down = (r == 4 ? ex_shift<0x105>(down) : ex_shift<0x101>(down)) + x[8 * kb + 7 - r];
-    }
-    up = ex_shift_rows<0x114, 0x3>(up);
-    down = ex_shift_rows<0x104, 0xC>(down);
-    // lanes below 32 take both halves' `up`, the others `down`, whose lanes 0 are `up`'s lanes 15
-    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(up), __float_as_uint(down), false, false);
-    const float v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
-    wave_lds_sync();
-    if (lane < 32) o[-16 * kb] += v;  // the two halves' entries overlap
-    wave_lds_sync();
-    if (lane >= 32 && f > 0) o[-16 * kb] += v;
+    up[kb] = x[8 * kb];
+    down[kb] = x[8 * kb + 7];
   }
-  wave_lds_sync();
+#pragma unroll
+  for (int r = 1; r < 8; ++r)
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      up[kb] = (r == 4 ? ex_shift<0x115>(up[kb]) : ex_shift<0x111>(up[kb])) + x[8 * kb + r];
+      down[kb] = (r == 4 ? ex_shift<0x105>(down[kb]) : ex_shift<0x101>(down[kb])) + x[8 * kb + 7 - r];
+    }
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    up[kb] = ex_shift_rows<0x111, 0xC>(ex_shift_rows<0x115, 0x3>(up[kb]));  // query 11 + 4 hf to 16
+    down[kb] = ex_shift_rows<0x104, 0xC>(down[kb]);                         // query 4 hf to 0
+  }
+  // Rows of 16 lanes by (query half hf, key half a): up of key half a and queries kb has the 16 entries from
+  // 16 (a - kb) - 16 on, down those from 16 (a - kb) on. As rows of entries from -32, -16, 0, 16 on:
+  // up[1] and down[0] added over hf are the four rows, and up[0] + down[1] belongs to the middle two.
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(up[1]), __float_as_uint(down[0]), false, false);
+  float w = up[0] + down[1];
+  w += ex_other_half(w);
+  const auto m = __builtin_amdgcn_permlane16_swap(__float_as_uint(w), __float_as_uint(w), false, false);
+  float v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  v += ex_rows_only<0x2>(__uint_as_float(m[0])) + ex_rows_only<0x4>(__uint_as_float(m[1]));
+  if (d.at != at) {
+    ex_diag_flush(d, lane);
+    d.pend = 0.f;
+  }
+  if (lane >= 32) d.dg[at + lane - 32] = v + d.pend;
+  d.pend = ex_other_half(v);
+  d.at = at - 32;
 }
 // Takes a wave's sums of a head out as a part of the bias gradient: far tiles' sums per lane (`left`: rel
 // <= -D, `right`: rel >= D) and the array, which is left as zeros. A bucket's entries are neighbours; four
 // lanes share those of a bucket.
-__device__ __forceinline__ void ex_put_buckets(const ExactParams& p, float* dg, int n, float left, float right, int64_t part,
+__device__ __forceinline__ void ex_put_buckets(const ExactParams& p, ExDiag& d, int n, float left, float right, int64_t part,
                                                int head, int lane_) {
   const int lane = ex_opaque(lane_);
+  float* dg = d.dg;
+  ex_diag_flush(d, lane);
   wave_lds_sync();
   left += ex_other_half(left);
   right += ex_other_half(right);
@@ -170,13 +202,13 @@ __device__ __forceinline__ float ex_row_dot(const ExRow<T>& a, const ExRow<T>& b
 // comes from large P, and is multiplied by them: the kernel of 64-row tiles leaves half tiles out of sum_j P k
 // whose P are all at most kSmallP (at 4 x 4096 tokens, 12 heads, all of them: dQ 317 us without this, 427
 // with every tile's product).
-template <typename T, bool BIAS>
+template <typename T, bool BIAS, int ST>
 __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
   extern __shared__ __align__(16) char smem[];
-  constexpr int ES = ExFmt<T>::ES, ST = kBwdStages<T>, TB = tile_bytes<T>();
+  constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>();
   const int n = 2 * p.D + 129;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  float* tb = reinterpret_cast<float*>(smem + kDqLds<T>);  // [Gp][n]
+  float* tb = reinterpret_cast<float*>(smem + kDqLds<T, ST>);  // [Gp][n]
   const int c = lane & 31, hf = lane >> 5;
   const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp;
   int bid = blockIdx.x;
@@ -301,16 +333,16 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
 // block's part of them (kv_splits). S = Q K^T and dP = dY V^T with the lane holding a key: P and dS
 // feed dV^T = dY^T P and dK^T = Q^T dS. A wave loads its tiles of Q, dY and row statistics straight
 // into LDS.
-template <typename T, bool BIAS>
+template <typename T, bool BIAS, int ST>
 __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int heads_at_once) {
   extern __shared__ __align__(16) char smem[];
-  constexpr int ES = ExFmt<T>::ES, ST = kBwdStages<T>, TB = tile_bytes<T>(), SB = kDkvStage<T>;
+  constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>(), SB = kDkvStage<T>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nkt = (p.nk + 31) / 32;
   int bid = blockIdx.x;
   const int c = lane & 31, hf = lane >> 5, n = 2 * p.D + 129;
-  float* dg = reinterpret_cast<float*>(smem + kDkvLds<T>) + wave * n;  // the wave's sums along diagonals
-  float* tb = reinterpret_cast<float*>(smem + kDkvLds<T>) + kExWaves * n;  // [heads_at_once][n]
+  ExDiag diag{reinterpret_cast<float*>(smem + kDkvLds<T, ST>) + wave * n, 0.f, -1};
+  float* tb = reinterpret_cast<float*>(smem + kDkvLds<T, ST>) + kExWaves * n;  // [heads_at_once][n]
   const int kt = bid % nkt;
   bid /= nkt;
   const int hk = bid % p.Hk;
@@ -332,7 +364,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
   float far_l = 0.f, far_r = 0.f;
   const int64_t part = ((int64_t)(split * p.B + b) * nkt + kt) * kExWaves + wave;
   if constexpr (BIAS)
-    for (int e = lane; e < n; e += 64) dg[e] = 0.f;
+    for (int e = lane; e < n; e += 64) diag.dg[e] = 0.f;
 
   for (int g0 = 0; g0 < p.G; g0 += heads_at_once) {
     const int ng = min(heads_at_once, p.G - g0), h0 = hk * p.G + g0;
@@ -390,7 +422,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
       int side = 0;
       if constexpr (BIAS) {
         for (const int h = idx / tiles.n; head < h; ++head) {
-          ex_put_buckets(p, dg, n, far_l, far_r, part, h0 + head, lane);
+          ex_put_buckets(p, diag, n, far_l, far_r, part, h0 + head, lane);
           far_l = far_r = 0.f;
         }
         const float* tl = tb + head * n + p.D + 64;
@@ -422,13 +454,13 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
       if constexpr (BIAS) {
         if (side < 0) far_l += ex_sum16(ds);
         else if (side > 0) far_r += ex_sum16(ds);
-        else ex_diagonals(ds, dg + p.D + 64 + kt * 32 - p0, lane);
+        else ex_diagonals(diag, ds, p.D + 64 + kt * 32 - p0, lane);
       }
       slot = slot == ST - 1 ? 0 : slot + 1;
     }
     if constexpr (BIAS)
       for (; head < ng; ++head) {
-        ex_put_buckets(p, dg, n, far_l, far_r, part, h0 + head, lane);
+        ex_put_buckets(p, diag, n, far_l, far_r, part, h0 + head, lane);
         far_l = far_r = 0.f;
       }
     wait_vmcnt<0>();
@@ -670,7 +702,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hf = lane >> 5, n = 2 * p.D + 129;
   const int nkt = (p.nk + 127) / 128;
-  float* dg = reinterpret_cast<float*>(smem + kDkvTilesLds) + wave * n;
+  ExDiag diag{reinterpret_cast<float*>(smem + kDkvTilesLds) + wave * n, 0.f, -1};
   float* tb = reinterpret_cast<float*>(smem + kDkvTilesLds) + kExWaves * n;
   int kt, pair;
   ex_block_pair(blockIdx.x, nkt, p.Hk * p.B * p.kv_splits, p.causal || p.window, kt, pair);
@@ -709,25 +741,36 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   };
   const ExRange whole = ex_whole_queries(p, kw, BIAS ? br.klen : 0x7fffffff);
   float fac = p.s2, add = 0.f, far_l = 0.f, far_r = 0.f;
-  int side = 0, diag = 0;  // where the half tile lies, and the entry of its first key and query
+  int side = 0, entry = 0;  // where the half tile lies, and the entry of its first key and query
   const float* tl = nullptr;
   const int64_t part = ((int64_t)(split * p.B + b) * nkt + kt) * kExWaves + wave;
   if constexpr (BIAS)
-    for (int e = lane; e < n; e += 64) dg[e] = 0.f;
+    for (int e = lane; e < n; e += 64) diag.dg[e] = 0.f;
+  // The bias of the half tile whose scores come next, read before they are there: near pairs' entries.
+  int next = 0;
+  f32x16_t bv;
+  auto peek = [&](int i0, const float* tn) __attribute__((always_inline)) {
+    const int q0 = br.pos + i0;
+    next = ex_bias_side(p, kw, q0, q0 + 31);
+    if (next == 0) {
+      const float* at = tn + (kw + ex_opaque(c) - q0 - 4 * hf);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) bv[r] = at[-((r & 3) + 8 * (r >> 2))];
+    }
+  };
   auto fix = [&](f32x16_t& s, int i0) __attribute__((always_inline)) {
     const int q0 = br.pos + i0;
     if constexpr (BIAS) {
-      side = ex_bias_side(p, kw, q0, q0 + 31);
-      diag = p.D + 64 + kw - q0;
+      side = next;
+      entry = p.D + 64 + kw - q0;
       fac = p.s2;
       add = 0.f;
       if (side != 0) {
         add = tl[side * p.D];
       } else {
         fac = 1.f;
-        const float* at = tl + (kw + ex_opaque(c) - q0 - 4 * hf);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = __fmaf_rn(s[r], p.s2, at[-((r & 3) + 8 * (r >> 2))]);
+        for (int r = 0; r < 16; ++r) s[r] = __fmaf_rn(s[r], p.s2, bv[r]);
       }
     }
     // rows past the last query add nothing, and keys past the last key only to the bias gradient
@@ -736,10 +779,10 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       ex_mask(s, queries, i0 + 4 * hf, q0 > 0);
     }
   };
-  // Half tile ch of ct: P and dS from (s, d); half tile nh of nt: S and dP into (sn, dn); (ft, fh): the one
-  // after that, whose start values take the place of (s, d).
+  // Half tile ch of ct: P and dS from (s, d); half tile nh of nt, of queries in on and bias table tn: S and dP into
+  // (sn, dn); (ft, fh): the one after that, whose start values take the place of (s, d).
   auto step = [&](f32x16_t& s, f32x16_t& d, f32x16_t& sn, f32x16_t& dn, const char* ct, int ch, const char* nt, int nh,
-                  const char* ft, int fh) __attribute__((always_inline)) {
+                  const char* ft, int fh, int in, const float* tn) __attribute__((always_inline)) {
     ExPair e{0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -770,9 +813,10 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       if (BIAS && i == 8) {
         if (side < 0) far_l += ex_sum16(d);
         else if (side > 0) far_r += ex_sum16(d);
-        else ex_diagonals(d, dg + diag, lane);
+        else ex_diagonals(diag, d, entry, lane);
       }
       if (i == 9) start(s, d, ft, fh);
+      if (BIAS && i == 10) peek(in, tn);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -785,12 +829,6 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     if (total > 0) {
     g = first / tiles.n;
     t = first % tiles.n;
-    if constexpr (BIAS) {
-      __syncthreads();
-      ex_fill_bias<uint16_t>(p, tb, h0, ng);
-      for (int k = 0; k < g; ++k) ex_put_buckets(p, dg, n, 0.f, 0.f, part, h0 + k, lane);
-      tl = tb + g * n + p.D + 64;
-    }
     // the next tile to load (head lg, tile lt), and how many
     int lg = g, lt = t, left = total;
     bool jump = true;
@@ -828,6 +866,12 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     __syncthreads();  // the buffers (and the bias tables) are this chunk's from here on
     load(0);
     load(1);
+    if constexpr (BIAS) {
+      ex_fill_bias<uint16_t>(p, tb, h0, ng);
+      for (int k = 0; k < g; ++k) ex_put_buckets(p, diag, n, 0.f, 0.f, part, h0 + k, lane);
+      tl = tb + g * n + p.D + 64;
+      lds_barrier();
+    }
     wait_vmcnt<4>();  // tile 0
     stage_barrier();
     start(s0, p0, smem, 0);
@@ -840,6 +884,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     start(s1, p1, smem, 1);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) fr[i] = read(i, smem, 1, nullptr, 0);
+    if constexpr (BIAS) peek(ex_tile_at(tiles, t) * 64, tl);
     int b0 = 0, b1 = 1, b2 = 2;  // buffers of the tile, the next one, the one after
 #pragma clang loop unroll(disable)
     for (int it = 0; it < total; ++it) {
@@ -847,11 +892,12 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       stage_barrier();
       load(b2);
       const char *ct = smem + b0 * kDkvTilesStage, *nt = smem + b1 * kDkvTilesStage;
-      const int i0 = ex_tile_at(tiles, t) * 64;
+      const bool last = t + 1 == tiles.n;  // the next tile is the next head's first
+      const int i0 = ex_tile_at(tiles, t) * 64, in = ex_tile_at(tiles, last ? 0 : t + 1) * 64;
       fix(s0, i0);
-      step(s0, p0, s1, p1, ct, 0, ct, 1, nt, 0);
+      step(s0, p0, s1, p1, ct, 0, ct, 1, nt, 0, i0 + 32, tl);
       fix(s1, i0 + 32);
-      step(s1, p1, s0, p0, ct, 1, nt, 0, nt, 1);
+      step(s1, p1, s0, p0, ct, 1, nt, 0, nt, 1, in, last && g + 1 < ng ? tl + n : tl);
       const int o = b0;
       b0 = b1;
       b1 = b2;
@@ -859,7 +905,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       if (++t == tiles.n) {
         t = 0;
         if constexpr (BIAS) {
-          ex_put_buckets(p, dg, n, far_l, far_r, part, h0 + g, lane);
+          ex_put_buckets(p, diag, n, far_l, far_r, part, h0 + g, lane);
           far_l = far_r = 0.f;
           tl += n;
         }
@@ -870,7 +916,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     }
     if constexpr (BIAS)
       for (; g < ng; ++g) {  // what is left of the part's last head, and the heads behind it
-        ex_put_buckets(p, dg, n, far_l, far_r, part, h0 + g, lane);
+        ex_put_buckets(p, diag, n, far_l, far_r, part, h0 + g, lane);
         far_l = far_r = 0.f;
       }
   }
@@ -936,14 +982,6 @@ __global__ __launch_bounds__(kExThreads) void k_exact_join_grads(ExactParams p, 
   }
 }
 
-constexpr size_t kMaxLds = 163840;  // of a block: a CU's
-
-template <typename K>
-hipError_t set_lds(K kernel, size_t lds) {
-  if (lds > kMaxLds) return hipErrorInvalidValue;
-  return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-}
-
 // bf16 in blocks of 128 rows where the blocks of 32 are more than the CUs, or, in a long loop, which is all a
 // block of 128 has on a CU then, twice as many (backward pass, 12 heads: 8 x 128 tokens, 384 blocks of 32,
 // 16.7 against 14.8 us; 4 x 256 22.4 and 18.6; 2 x 512 26.1 and 31.9; 1 x 1024 34.4 and 44.1; 2 x 256, 192
@@ -961,7 +999,7 @@ bool dkv_in_tiles(const ExactParams& p) {
 
 // The largest table (and a wave's sums along diagonals, as long) fits beside the tiles.
 constexpr size_t kMaxTable = (2 * kMaxBiasDistance + 129) * 4;
-static_assert(kDkvLds<float> + (kExWaves + 1) * kMaxTable <= kMaxLds && kDkvLds<uint16_t> + (kExWaves + 1) * kMaxTable <= kMaxLds &&
+static_assert(kDkvLds<float, 2> + (kExWaves + 1) * kMaxTable <= kMaxLds && kDkvLds<uint16_t, 2> + (kExWaves + 1) * kMaxTable <= kMaxLds &&
               kDkvTilesLds + (kExWaves + 1) * kMaxTable <= kMaxLds / 2, "LDS of a block");
 
 template <typename T, bool BIAS>
@@ -971,22 +1009,29 @@ hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
   if constexpr (ExFmt<T>::ES == 2) {
     if (dq_in_tiles(p)) {
       const size_t lds = 6 * kTile64 + table;
-      if ((e = set_lds(k_exact_dq_tiles<BIAS>, lds)) != hipSuccess) return e;
+      if ((e = exact_set_lds<k_exact_dq_tiles<BIAS>>(lds)) != hipSuccess) return e;
       const int64_t blocks = (int64_t)((p.nq + 127) / 128) * p.H * p.B;
       hipLaunchKernelGGL((k_exact_dq_tiles<BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
       return hipGetLastError();
     }
   }
-  const size_t lds = kDqLds<T> + table * p.Gp;
-  if ((e = set_lds(k_exact_dq<T, BIAS>, lds)) != hipSuccess) return e;
   const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
-  hipLaunchKernelGGL((k_exact_dq<T, BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
+  const size_t one = kDqLds<T, 1> + table * p.Gp, two = kDqLds<T, 2> + table * p.Gp;
+  if constexpr (ExFmt<T>::ES == 4) {  // as the forward pass
+    if (blocks > device_cus()) {
+      if ((e = exact_set_lds<k_exact_dq<T, BIAS, 1>>(one)) != hipSuccess) return e;
+      hipLaunchKernelGGL((k_exact_dq<T, BIAS, 1>), dim3((unsigned)blocks), dim3(kExThreads), one, s, p);
+      return hipGetLastError();
+    }
+  }
+  if ((e = exact_set_lds<k_exact_dq<T, BIAS, 2>>(two)) != hipSuccess) return e;
+  hipLaunchKernelGGL((k_exact_dq<T, BIAS, 2>), dim3((unsigned)blocks), dim3(kExThreads), two, s, p);
   return hipGetLastError();
 }
 
 // A block's tiles and its waves' sums along diagonals in LDS, then the bias tables of as many heads as fit.
-template <bool BIAS, typename K>
-hipError_t launch_dkv_kernel(K kernel, const ExactParams& p, int keys, size_t base, hipStream_t s) {
+template <auto K, bool BIAS>
+hipError_t launch_dkv_kernel(const ExactParams& p, int keys, size_t base, hipStream_t s) {
   const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
   base += kExWaves * table;
   int heads = p.G;
@@ -995,18 +1040,23 @@ hipError_t launch_dkv_kernel(K kernel, const ExactParams& p, int keys, size_t ba
     heads = (int)std::min<size_t>(heads, (room - base) / table);
   }
   const size_t lds = base + table * heads;
-  const hipError_t e = set_lds(kernel, lds);
+  const hipError_t e = exact_set_lds<K>(lds);
   if (e != hipSuccess) return e;
   const int64_t blocks = (int64_t)((p.nk + keys - 1) / keys) * p.Hk * p.B * p.kv_splits;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
+  hipLaunchKernelGGL(K, dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
   return hipGetLastError();
 }
 
 template <typename T, bool BIAS>
 hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
   hipError_t e = hipErrorInvalidValue;
-  if (!dkv_in_tiles(p)) e = launch_dkv_kernel<BIAS>(k_exact_dkv<T, BIAS>, p, 32, kDkvLds<T>, s);
-  else if constexpr (ExFmt<T>::ES == 2) e = launch_dkv_kernel<BIAS>(k_exact_dkv_tiles<BIAS>, p, 128, kDkvTilesLds, s);
+  if (!dkv_in_tiles(p)) {
+    e = hipErrorNotReady;
+    if constexpr (ExFmt<T>::ES == 4)  // (as the forward pass)
+      if ((int64_t)((p.nk + 31) / 32) * p.Hk * p.B * p.kv_splits > device_cus())
+        e = launch_dkv_kernel<k_exact_dkv<T, BIAS, 1>, BIAS>(p, 32, kDkvLds<T, 1>, s);
+    if (e == hipErrorNotReady) e = launch_dkv_kernel<k_exact_dkv<T, BIAS, 2>, BIAS>(p, 32, kDkvLds<T, 2>, s);
+  } else if constexpr (ExFmt<T>::ES == 2) e = launch_dkv_kernel<k_exact_dkv_tiles<BIAS>, BIAS>(p, 128, kDkvTilesLds, s);
   if (e != hipSuccess) return e;
   const int sums = BIAS ? (p.buckets * p.H + kExWaves - 1) / kExWaves : 0;
   const int64_t rows = p.kv_splits > 1 ? ((int64_t)p.B * p.nk * p.Hk * (kDHead / 4) + kExThreads - 1) / kExThreads : 0;

@@ -49,14 +49,14 @@ __device__ __forceinline__ void ex_softmax_step(ExState& s, f32x16_t& x) {
 // once for them. The key tiles are dealt out to the block's four waves and to `splits` blocks; a
 // wave loads its own tiles straight into LDS ahead of their use and waits for nobody until the
 // end, where the waves' states (and the blocks', in k_exact_join) are joined in a fixed order.
-template <typename T> constexpr int kRowStages = ExFmt<T>::ES == 2 ? 2 : 1;
-template <typename T> constexpr int kRowLds = kExWaves * kRowStages<T> * 2 * tile_bytes<T>();
+template <typename T, int ST> constexpr int kRowLds = kExWaves * ST * 2 * tile_bytes<T>();
 
-template <typename T, bool BIAS>
+// ST: tiles in LDS per wave, all but one of them on their way.
+template <typename T, bool BIAS, int ST>
 __global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
   extern __shared__ __align__(16) char smem[];
-  constexpr int ES = ExFmt<T>::ES, ST = kRowStages<T>, TB = tile_bytes<T>();
-  float* tb = reinterpret_cast<float*>(smem + kRowLds<T>);
+  constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>();
+  float* tb = reinterpret_cast<float*>(smem + kRowLds<T, ST>);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hf = lane >> 5;
   const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp;
@@ -481,20 +481,31 @@ template <bool BIAS, int MT>
 hipError_t launch_tiles(const ExactParams& p, hipStream_t s) {
   const size_t lds = 6 * kTile64 + (BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0);
   const int64_t blocks = (int64_t)((p.nq + 128 * MT - 1) / (128 * MT)) * p.H * p.B;
+  static_assert(6 * kTile64 + (2 * kMaxBiasDistance + 129) * 4 <= 65536 - 512, "LDS that needs no leave");
   hipLaunchKernelGGL((k_exact_tiles<BIAS, MT>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
   return hipGetLastError();
 }
 
-template <typename T, bool BIAS>
-hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
-  const size_t lds = kRowLds<T> + (BIAS ? (size_t)p.Gp * exact_bias_entries(p.D) * 4 : 0);
-  hipError_t e = hipFuncSetAttribute((const void*)k_exact_rows<T, BIAS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+template <typename T, bool BIAS, int ST>
+hipError_t launch_rows_of(const ExactParams& p, hipStream_t s) {
+  const size_t lds = kRowLds<T, ST> + (BIAS ? (size_t)p.Gp * exact_bias_entries(p.D) * 4 : 0);
+  hipError_t e = exact_set_lds<k_exact_rows<T, BIAS, ST>>(lds);
   if (e != hipSuccess) return e;
   const int64_t rows = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
-  hipLaunchKernelGGL((k_exact_rows<T, BIAS>), dim3((unsigned)(rows * p.splits)), dim3(kExThreads), lds, s, p);
+  hipLaunchKernelGGL((k_exact_rows<T, BIAS, ST>), dim3((unsigned)(rows * p.splits)), dim3(kExThreads), lds, s, p);
   if ((e = hipGetLastError()) != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL((k_exact_join<T>), dim3((unsigned)(((int64_t)p.B * p.H * p.nq + kExWaves - 1) / kExWaves)), dim3(kExThreads), 0, s, p);
   return hipGetLastError();
+}
+
+// bf16: two tiles, 64 KB of LDS for a block, two of them to a CU. float32, whose tiles are twice as large: two
+// where every block has a CU of its own, else one and two blocks to a CU, which cover each other's loads
+// (forward, 12 heads: 2 x 333 tokens, one block to a CU, 14.6 against 15.5 us; 32 x 128, six, 48 against 36).
+template <typename T, bool BIAS>
+hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
+  if constexpr (ExFmt<T>::ES == 4)
+    if (exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B * p.splits > device_cus()) return launch_rows_of<T, BIAS, 1>(p, s);
+  return launch_rows_of<T, BIAS, 2>(p, s);
 }
 
 }  // namespace
@@ -502,7 +513,7 @@ hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
 // Heads side by side in the kernels of 32 rows: a key head's whole group, unless its bias tables do not
 // fit beside the tiles.
 int exact_group(const ExactParams& p) {
-  return !p.table || (int64_t)p.G * exact_bias_entries(p.D) * 4 <= 163840 - kRowLds<float> ? p.G : 1;
+  return !p.table || (int64_t)p.G * exact_bias_entries(p.D) * 4 <= (int64_t)kMaxLds - kRowLds<float, 2> ? p.G : 1;
 }
 
 // bf16 in blocks of 128 queries or more: where the blocks of 32 rows are more than the CUs (forward, 12
