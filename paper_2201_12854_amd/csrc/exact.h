@@ -58,16 +58,16 @@ inline int64_t exact_row_tiles(int64_t nq, int64_t Gp) { return (nq * Gp + 31) /
 
 constexpr size_t kMaxLds = 163840;  // of a block: a CU's
 
-// Allows kernel K that much LDS, once per device; an error where `lds` is more.
-template <auto K>
+// Allows kernel K that much LDS less STATIC of its own, once per device; an error where `lds` is more.
+template <auto K, int STATIC = 0>
 hipError_t exact_set_lds(size_t lds) {
   static std::atomic<int> allowed[64];
   int dev = 0;
-  if (lds > kMaxLds) return hipErrorInvalidValue;
+  if (lds > kMaxLds - STATIC) return hipErrorInvalidValue;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return hipErrorInvalidDevice;
   if (allowed[dev].load(std::memory_order_acquire)) return hipSuccess;
   // idempotent: threads racing here all set the same attribute before any of them launches
-  const hipError_t e = hipFuncSetAttribute((const void*)K, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxLds);
+  const hipError_t e = hipFuncSetAttribute((const void*)K, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxLds - STATIC);
   if (e == hipSuccess) allowed[dev].store(1, std::memory_order_release);
   return e;
 }

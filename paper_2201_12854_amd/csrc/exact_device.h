@@ -396,12 +396,12 @@ __device__ __forceinline__ ExTiles ex_tiles(int lo, int hi, int extra) {  // of 
   }
   return t;
 }
-// Key tiles of the queries at positions pmin .. pmax.
+// Key tiles of the queries at positions pmin .. pmax; `all`: a global query among them counts.
 template <int TILE = 32>
-__device__ __forceinline__ ExTiles ex_key_tiles(const ExactParams& p, int pmin, int pmax, int klen) {
+__device__ __forceinline__ ExTiles ex_key_tiles(const ExactParams& p, int pmin, int pmax, int klen, bool all = true) {
   int lo = 0, hi = klen - 1, extra = -1;
   if (p.causal) hi = min(hi, pmax);
-  if (p.window && (p.causal || pmin > 0 || pmax < 0)) {  // no global query with keys of its own
+  if (p.window && (!all || p.causal || pmin > 0 || pmax < 0)) {  // no global query with keys of its own
     lo = max(0, pmin - p.half);
     hi = min(hi, pmax + p.half);
     if (klen > 0 && (!p.causal || pmax >= 0)) extra = 0;
@@ -420,6 +420,12 @@ __device__ __forceinline__ ExTiles ex_query_tiles(const ExactParams& p, const Ex
     if (!p.causal && -r.pos >= 0 && -r.pos < r.qlen) extra = -r.pos;
   }
   return ex_tiles<TILE>(lo, hi, extra);
+}
+// Under a window the kernels of 128 rows leave the 32 rows around a global row, whose way over the keys (or
+// queries) is far longer than the others', to blocks of their own at the grid's beginning, whose four waves
+// share it. The first of those 32 query rows, -1 if there is none: causal queries have no such row.
+__device__ __forceinline__ int ex_global_rows(const ExactParams& p, const ExRow0& r) {
+  return p.window && !p.causal && -r.pos >= 0 && -r.pos < r.qlen ? -r.pos / 32 * 32 : -1;
 }
 // Where part k of n begins among `all` tiles.
 __device__ __forceinline__ int ex_part(int all, int k, int n) { return (int)((int64_t)all * k / n); }

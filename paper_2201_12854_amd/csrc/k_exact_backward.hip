@@ -203,25 +203,19 @@ __device__ __forceinline__ float ex_row_dot(const ExRow<T>& a, const ExRow<T>& b
 // whose P are all at most kSmallP (at 4 x 4096 tokens, 12 heads, all of them: dQ 317 us without this, 427
 // with every tile's product).
 template <typename T, bool BIAS, int ST>
-__global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
-  extern __shared__ __align__(16) char smem[];
+__device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, int vt, int hx, int b, int Gp) {
   constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>();
   const int n = 2 * p.D + 129;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float* tb = reinterpret_cast<float*>(smem + kDqLds<T, ST>);  // [Gp][n]
   const int c = lane & 31, hf = lane >> 5;
-  const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp;
-  int bid = blockIdx.x;
-  const int vt = bid % nvt;
-  bid /= nvt;
-  const int hx = bid % Hx, b = bid / Hx;
   const ExRow0 br = ex_batch_row(p, b);
-  const int hk = hx * p.Gp / p.G;
+  const int hk = hx * Gp / p.G;
 
-  const int v = vt * 32 + c, i = v / p.Gp, g = v % p.Gp, head = hx * p.Gp + g;
+  const int v = vt * 32 + c, i = v / Gp, g = v % Gp, head = hx * Gp + g;
   const bool live = i < br.qlen;
-  const int imin = vt * 32 / p.Gp, imax = min((vt * 32 + 31) / p.Gp, br.qlen - 1);
-  const int pmin = br.pos + imin, pmax = br.pos + imax, pend = br.pos + (vt * 32 + 31) / p.Gp;
+  const int imin = vt * 32 / Gp, imax = min((vt * 32 + 31) / Gp, br.qlen - 1);
+  const int pmin = br.pos + imin, pmax = br.pos + imax, pend = br.pos + (vt * 32 + 31) / Gp;
   const ExTiles tiles = imax >= imin ? ex_key_tiles(p, pmin, pmax, br.klen) : ExTiles{-1, 0, 0};
 
   const char* Kb = static_cast<const char*>(p.K.data) + (b * p.K.batch + hk * kDHead) * ES;
@@ -254,7 +248,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
   const float* tl = nullptr;
   float rest = 0.f;  // sum of dS
   if constexpr (BIAS) {
-    ex_fill_bias<T>(p, tb, hx * p.Gp, p.Gp);
+    ex_fill_bias<T>(p, tb, hx * Gp, Gp);
     __syncthreads();
     tl = tb + g * n + p.D + 64;
   }
@@ -321,11 +315,18 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     const int row = (threadIdx.x >> 4) + half * 16, col = (threadIdx.x & 15) * 4;
-    const int vr = vt * 32 + row, ir = vr / p.Gp;
+    const int vr = vt * 32 + row, ir = vr / Gp;
     if (ir < p.nq)
-      ex_store4(static_cast<T*>(p.dQ.data) + b * p.dQ.batch + ir * p.dQ.row + (hx * p.Gp + vr % p.Gp) * kDHead + col,
+      ex_store4(static_cast<T*>(p.dQ.data) + b * p.dQ.batch + ir * p.dQ.row + (hx * Gp + vr % Gp) * kDHead + col,
                 ex_join_sums(ys, row, col, p.scale));
   }
+}
+
+template <typename T, bool BIAS, int ST>
+__global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
+  extern __shared__ __align__(16) char smem[];
+  const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp, bid = blockIdx.x / nvt;
+  ex_dq_block<T, BIAS, ST>(p, smem, blockIdx.x % nvt, bid % Hx, bid / Hx, p.Gp);
 }
 
 // ------------------------------------------------------------------ dK, dV
@@ -334,20 +335,13 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
 // feed dV^T = dY^T P and dK^T = Q^T dS. A wave loads its tiles of Q, dY and row statistics straight
 // into LDS.
 template <typename T, bool BIAS, int ST>
-__global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int heads_at_once) {
-  extern __shared__ __align__(16) char smem[];
+__device__ __forceinline__ void ex_dkv_block(const ExactParams& p, char* smem, int kt, int hk, int b, int split, int splits,
+                                             int64_t part, int heads_at_once) {
   constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>(), SB = kDkvStage<T>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int nkt = (p.nk + 31) / 32;
-  int bid = blockIdx.x;
   const int c = lane & 31, hf = lane >> 5, n = 2 * p.D + 129;
   ExDiag diag{reinterpret_cast<float*>(smem + kDkvLds<T, ST>) + wave * n, 0.f, -1};
   float* tb = reinterpret_cast<float*>(smem + kDkvLds<T, ST>) + kExWaves * n;  // [heads_at_once][n]
-  const int kt = bid % nkt;
-  bid /= nkt;
-  const int hk = bid % p.Hk;
-  bid /= p.Hk;
-  const int b = bid % p.B, split = bid / p.B;
   const ExRow0 br = ex_batch_row(p, b);
   const int j = kt * 32 + c, jmax = min(kt * 32 + 31, br.klen - 1);
   const ExTiles tiles = ex_query_tiles(p, br, kt * 32, jmax);
@@ -360,9 +354,9 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
   const ExRow<T> vf = live ? ex_global_row<T>(vrow, hf) : ex_zero_row<T>();
   f32x16_t dk[2] = {ex_zero16(), ex_zero16()}, dv[2] = {ex_zero16(), ex_zero16()};
   const uint32_t lds = lds_addr(smem) + (uint32_t)wave * ST * SB;
-  const int all = tiles.n * p.G, from = ex_part(all, split, p.kv_splits), to_ = ex_part(all, split + 1, p.kv_splits);
+  const int all = tiles.n * p.G, from = ex_part(all, split, splits), to_ = ex_part(all, split + 1, splits);
   float far_l = 0.f, far_r = 0.f;
-  const int64_t part = ((int64_t)(split * p.B + b) * nkt + kt) * kExWaves + wave;
+  part += wave;
   if constexpr (BIAS)
     for (int e = lane; e < n; e += 64) diag.dg[e] = 0.f;
 
@@ -476,7 +470,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
     for (int half = 0; half < 2; ++half) {
       const int row = (threadIdx.x >> 4) + half * 16, col = (threadIdx.x & 15) * 4, jr = kt * 32 + row;
       if (jr >= p.nk) continue;
-      if (p.kv_splits > 1) {
+      if (splits > 1) {
         const int64_t at = (((int64_t)(split * p.B + b) * p.nk + jr) * p.Hk + hk) * kDHead + col;
         ex_store4((which ? p.part_dv : p.part_dk) + at, ex_join_sums(ys, row, col, 1.f));
       } else {
@@ -487,6 +481,19 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
       }
     }
   }
+}
+
+template <typename T, bool BIAS, int ST>
+__global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int heads_at_once) {
+  extern __shared__ __align__(16) char smem[];
+  const int nkt = (p.nk + 31) / 32;
+  int bid = blockIdx.x;
+  const int kt = bid % nkt;
+  bid /= nkt;
+  const int hk = bid % p.Hk;
+  bid /= p.Hk;
+  const int64_t part = ((int64_t)bid * nkt + kt) * kExWaves;  // bid: split * B + batch row
+  ex_dkv_block<T, BIAS, ST>(p, smem, kt, hk, bid % p.B, bid / p.B, p.kv_splits, part, heads_at_once);
 }
 
 // ------------------------------------------------------------------ tiles of 64 rows, bf16
@@ -517,7 +524,7 @@ __device__ __forceinline__ ExPair ex_pair(const f32x16_t& s, int j, float fac, f
 
 constexpr float kSmallP = 0x1p-6f;
 
-template <bool BIAS>
+template <bool BIAS, bool WIN>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_dq_tiles(ExactParams p) {
   extern __shared__ __align__(16) char smem[];  // three K tiles, three V tiles, the bias table
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -525,13 +532,23 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   float* tb = reinterpret_cast<float*>(smem + 6 * kTile64);
   int qt, pair;
   const int nqt = (p.nq + 127) / 128;
-  ex_block_pair(blockIdx.x, nqt, p.H * p.B, p.causal || p.window, qt, pair);
+  int bid = blockIdx.x;
+  if constexpr (WIN) {  // the first blocks: the rows around a global query
+    if (bid < p.H * p.B) {
+      const int first = ex_global_rows(p, ex_batch_row(p, bid / p.H));
+      if (first >= 0) ex_dq_block<uint16_t, BIAS, 2>(p, smem, first / 32, bid % p.H, bid / p.H, 1);
+      return;
+    }
+    bid -= p.H * p.B;
+  }
+  ex_block_pair(bid, nqt, p.H * p.B, p.causal || p.window, qt, pair);
   if (p.causal) qt = nqt - 1 - qt;  // the longest rows first
   const int h = pair % p.H, b = pair / p.H, hk = h / p.G;
   const ExRow0 br = ex_batch_row(p, b);
   const int qw = qt * 128 + wave * 32, i = qw + c;
-  const int last = min(qt * 128 + 128, br.qlen) - 1;
-  const ExTiles tiles = last >= qt * 128 ? ex_key_tiles<64>(p, br.pos + qt * 128, br.pos + last, br.klen) : ExTiles{-1, 0, 0};
+  const int global = WIN ? ex_global_rows(p, br) : -1;
+  const int first = qt * 128 + (WIN && global == qt * 128 ? 32 : 0), last = min(qt * 128 + 128, br.qlen) - 1;
+  const ExTiles tiles = last >= first ? ex_key_tiles<64>(p, br.pos + first, br.pos + last, br.klen, !WIN) : ExTiles{-1, 0, 0};
   const ExRange whole = ex_whole_keys(p, br.pos + qw, br.pos + min(qw + 32, br.qlen) - 1, br.klen);
 
   const char* Kb = static_cast<const char*>(p.K.data) + (b * p.K.batch + hk * kDHead) * 2;
@@ -686,9 +703,10 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
     for (int r = 0; r < 16; ++r) dq[cc][r] = fmaf(-rest, pk[cc][r], dq[cc][r]);
-  if (hf == 0 && i < p.nq) ex_put_stat<uint16_t>(p, ((int64_t)b * p.H + h) * p.nq + i, cr, D);
   wait_vmcnt<0>();  // no load is under way into what is written next
   __syncthreads();
+  if (WIN && qw == global) return;  // another block has these rows
+  if (hf == 0 && i < p.nq) ex_put_stat<uint16_t>(p, ((int64_t)b * p.H + h) * p.nq + i, cr, D);
   char* out = static_cast<char*>(p.dQ.data) + (b * p.dQ.batch + (int64_t)qw * p.dQ.row + hcol) * 2;
   ex_store_rows32(smem + wave * 32 * 144, dq, p.scale, out, p.dQ.row * 2, p.nq - qw, lane);
 }
@@ -696,7 +714,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
 constexpr int kDkvTilesStage = 2 * kTile64 + 512;  // Q, dY, two planes of 64 statistics
 constexpr int kDkvTilesLds = 3 * kDkvTilesStage;
 
-template <bool BIAS>
+template <bool BIAS, bool WIN>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_dkv_tiles(ExactParams p, int heads_at_once) {
   extern __shared__ __align__(16) char smem[];  // three stages, sums along diagonals, the bias tables of `heads_at_once` heads
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -705,11 +723,20 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   ExDiag diag{reinterpret_cast<float*>(smem + kDkvTilesLds) + wave * n, 0.f, -1};
   float* tb = reinterpret_cast<float*>(smem + kDkvTilesLds) + kExWaves * n;
   int kt, pair;
-  ex_block_pair(blockIdx.x, nkt, p.Hk * p.B * p.kv_splits, p.causal || p.window, kt, pair);
+  int bid = blockIdx.x;
+  if constexpr (WIN) {  // the first blocks: the keys around the global one (kv_splits is 1)
+    if (bid < p.Hk * p.B) {
+      const int64_t part = ((int64_t)p.B * nkt + bid / p.Hk) * kExWaves;
+      ex_dkv_block<uint16_t, BIAS, 2>(p, smem, 0, bid % p.Hk, bid / p.Hk, 0, 1, part, heads_at_once);
+      return;
+    }
+    bid -= p.Hk * p.B;
+  }
+  ex_block_pair(bid, nkt, p.Hk * p.B * p.kv_splits, p.causal || p.window, kt, pair);
   const int hk = pair % p.Hk, b = pair / p.Hk % p.B, split = pair / (p.Hk * p.B);
   const ExRow0 br = ex_batch_row(p, b);
   const int kw = kt * 128 + wave * 32, j = kw + c;
-  const ExTiles tiles = ex_query_tiles<64>(p, br, kt * 128, min(kt * 128 + 128, br.klen) - 1);
+  const ExTiles tiles = ex_query_tiles<64>(p, br, kt * 128 + (WIN && kt == 0 ? 32 : 0), min(kt * 128 + 128, br.klen) - 1);
 
   ExRow<uint16_t> kf = ex_zero_row<uint16_t>(), vf = kf;
   if (j < br.klen) {
@@ -739,7 +766,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       d[4 * k] = u.x, d[4 * k + 1] = u.y, d[4 * k + 2] = u.z, d[4 * k + 3] = u.w;
     }
   };
-  const ExRange whole = ex_whole_queries(p, kw, BIAS ? br.klen : 0x7fffffff);
+  const bool mine = !WIN || kw > 0;  // another block has the first 32 keys
+  const ExRange whole = ex_whole_queries(p, kw, !mine ? 0 : BIAS ? br.klen : 0x7fffffff);
   float fac = p.s2, add = 0.f, far_l = 0.f, far_r = 0.f;
   int side = 0, entry = 0;  // where the half tile lies, and the entry of its first key and query
   const float* tl = nullptr;
@@ -775,7 +803,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     }
     // rows past the last query add nothing, and keys past the last key only to the bias gradient
     if (__builtin_expect(!ex_has(whole, q0), 0)) {
-      const ExSpan queries = ex_queries_of(p, br, kw + ex_opaque(c));
+      const ExSpan queries = mine ? ex_queries_of(p, br, kw + ex_opaque(c)) : ex_span(0, -1, -1);
       ex_mask(s, queries, i0 + 4 * hf, q0 > 0);
     }
   };
@@ -921,6 +949,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       }
   }
   __syncthreads();
+  if (!mine) return;
   if (p.kv_splits > 1) {
     if (j < p.nk) {
       const int64_t at = (((int64_t)(split * p.B + b) * p.nk + j) * p.Hk + hk) * kDHead + 4 * hf;
@@ -1008,10 +1037,14 @@ hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
   hipError_t e;
   if constexpr (ExFmt<T>::ES == 2) {
     if (dq_in_tiles(p)) {
-      const size_t lds = 6 * kTile64 + table;
-      if ((e = exact_set_lds<k_exact_dq_tiles<BIAS>>(lds)) != hipSuccess) return e;
       const int64_t blocks = (int64_t)((p.nq + 127) / 128) * p.H * p.B;
-      hipLaunchKernelGGL((k_exact_dq_tiles<BIAS>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
+      if (p.window && !p.causal) {
+        const size_t lds = kDqLds<T, 2> + table;
+        if ((e = exact_set_lds<k_exact_dq_tiles<BIAS, true>>(lds)) != hipSuccess) return e;
+        hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, true>), dim3((unsigned)(blocks + p.H * p.B)), dim3(kExThreads), lds, s, p);
+      } else {
+        hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, false>), dim3((unsigned)blocks), dim3(kExThreads), 6 * kTile64 + table, s, p);
+      }
       return hipGetLastError();
     }
   }
@@ -1031,7 +1064,7 @@ hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
 
 // A block's tiles and its waves' sums along diagonals in LDS, then the bias tables of as many heads as fit.
 template <auto K, bool BIAS>
-hipError_t launch_dkv_kernel(const ExactParams& p, int keys, size_t base, hipStream_t s) {
+hipError_t launch_dkv_kernel(const ExactParams& p, int keys, size_t base, hipStream_t s, int more = 0) {
   const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
   base += kExWaves * table;
   int heads = p.G;
@@ -1042,7 +1075,7 @@ hipError_t launch_dkv_kernel(const ExactParams& p, int keys, size_t base, hipStr
   const size_t lds = base + table * heads;
   const hipError_t e = exact_set_lds<K>(lds);
   if (e != hipSuccess) return e;
-  const int64_t blocks = (int64_t)((p.nk + keys - 1) / keys) * p.Hk * p.B * p.kv_splits;
+  const int64_t blocks = (int64_t)((p.nk + keys - 1) / keys) * p.Hk * p.B * p.kv_splits + more;
   hipLaunchKernelGGL(K, dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
   return hipGetLastError();
 }
@@ -1056,7 +1089,10 @@ hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
       if ((int64_t)((p.nk + 31) / 32) * p.Hk * p.B * p.kv_splits > device_cus())
         e = launch_dkv_kernel<k_exact_dkv<T, BIAS, 1>, BIAS>(p, 32, kDkvLds<T, 1>, s);
     if (e == hipErrorNotReady) e = launch_dkv_kernel<k_exact_dkv<T, BIAS, 2>, BIAS>(p, 32, kDkvLds<T, 2>, s);
-  } else if constexpr (ExFmt<T>::ES == 2) e = launch_dkv_kernel<k_exact_dkv_tiles<BIAS>, BIAS>(p, 128, kDkvTilesLds, s);
+  } else if constexpr (ExFmt<T>::ES == 2) {
+    if (p.window) e = launch_dkv_kernel<k_exact_dkv_tiles<BIAS, true>, BIAS>(p, 128, kDkvLds<T, 2>, s, p.Hk * p.B);
+    else e = launch_dkv_kernel<k_exact_dkv_tiles<BIAS, false>, BIAS>(p, 128, kDkvTilesLds, s);
+  }
   if (e != hipSuccess) return e;
   const int sums = BIAS ? (p.buckets * p.H + kExWaves - 1) / kExWaves : 0;
   const int64_t rows = p.kv_splits > 1 ? ((int64_t)p.B * p.nk * p.Hk * (kDHead / 4) + kExThreads - 1) / kExThreads : 0;
@@ -1078,6 +1114,7 @@ hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
 // where that saves more than the join takes.
 int exact_kv_splits(const ExactParams& p) {
   const bool big = dkv_in_tiles(p);
+  if (big && p.window) return 1;
   const int64_t blocks = (int64_t)((p.nk + (big ? 127 : 31)) / (big ? 128 : 32)) * p.Hk * p.B;
   const int64_t tiles = (int64_t)p.G * ((p.nq + (big ? 63 : 31)) / (big ? 64 : 32));
   const int64_t n = std::min((big ? 2 : 1) * device_cus() / blocks, tiles / (big ? 16 : kExWaves));
@@ -1085,7 +1122,8 @@ int exact_kv_splits(const ExactParams& p) {
 }
 
 int64_t exact_bias_parts(const ExactParams& p) {  // a part per wave of k_exact_dkv
-  return (int64_t)p.kv_splits * p.B * ((p.nk + (dkv_in_tiles(p) ? 127 : 31)) / (dkv_in_tiles(p) ? 128 : 32)) * kExWaves;
+  if (!dkv_in_tiles(p)) return (int64_t)p.kv_splits * p.B * ((p.nk + 31) / 32) * kExWaves;
+  return (int64_t)p.B * (p.kv_splits * ((p.nk + 127) / 128) + (p.window ? 1 : 0)) * kExWaves;
 }
 
 hipError_t launch_exact_backward(const ExactParams& p, hipStream_t s) {

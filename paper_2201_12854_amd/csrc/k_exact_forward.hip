@@ -53,32 +53,26 @@ template <typename T, int ST> constexpr int kRowLds = kExWaves * ST * 2 * tile_b
 
 // ST: tiles in LDS per wave, all but one of them on their way.
 template <typename T, bool BIAS, int ST>
-__global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
-  extern __shared__ __align__(16) char smem[];
+__device__ __forceinline__ void ex_rows_block(const ExactParams& p, char* smem, int vt, int hx, int b, int split, int splits,
+                                              int Gp) {
   constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>();
   float* tb = reinterpret_cast<float*>(smem + kRowLds<T, ST>);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hf = lane >> 5;
-  const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp;
-  int bid = blockIdx.x;
-  const int vt = bid % nvt;
-  bid /= nvt;
-  const int hx = bid % Hx;
-  bid /= Hx;
-  const int b = bid % p.B, split = bid / p.B;
+  const int nvt = (int)((p.nq * Gp + 31) / 32), Hx = p.H / Gp;
   const ExRow0 br = ex_batch_row(p, b);
-  const int hk = hx * p.Gp / p.G;
+  const int hk = hx * Gp / p.G;
 
-  const int v = vt * 32 + c, i = v / p.Gp, g = v % p.Gp, head = hx * p.Gp + g;
+  const int v = vt * 32 + c, i = v / Gp, g = v % Gp, head = hx * Gp + g;
   const bool live = i < br.qlen;
-  const int imin = vt * 32 / p.Gp, imax = min((vt * 32 + 31) / p.Gp, br.qlen - 1);
+  const int imin = vt * 32 / Gp, imax = min((vt * 32 + 31) / Gp, br.qlen - 1);
   const int pmin = br.pos + imin, pmax = br.pos + imax;
   const ExTiles tiles = imax >= imin ? ex_key_tiles(p, pmin, pmax, br.klen) : ExTiles{-1, 0, 0};
 
   const char* Kb = static_cast<const char*>(p.K.data) + (b * p.K.batch + hk * kDHead) * ES;
   const char* Vb = static_cast<const char*>(p.V.data) + (b * p.V.batch + hk * kDHead) * ES;
   const uint32_t lds = lds_addr(smem) + (uint32_t)wave * ST * 2 * TB;
-  const int step = kExWaves * p.splits;
+  const int step = kExWaves * splits;
   auto load = [&](int idx, int slot) __attribute__((always_inline)) {  // past the last tile: zeros
     const int k0 = ex_tile_at(tiles, idx) * 32, limit = idx < tiles.n ? br.klen : 0;
     ex_load_tile<T>(ex_rsrc(Kb, p.K.row * ES, k0, limit, ExFmt<T>::RB), (int)p.K.row * ES, lds + slot * 2 * TB, lane);
@@ -95,7 +89,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
   const ExSpan keys = ex_keys_of(p, pos, br.klen);
   const float* tl = nullptr;
   if constexpr (BIAS) {
-    ex_fill_bias<T>(p, tb, hx * p.Gp, p.Gp);
+    ex_fill_bias<T>(p, tb, hx * Gp, Gp);
     __syncthreads();
     tl = tb + g * (2 * p.D + 129) + p.D + 64;
   }
@@ -114,7 +108,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
     const int k0 = ex_tile_at(tiles, idx) * 32;
     f32x16_t x = ex_rows_product<T>(kt, q, c, hf);
     if constexpr (BIAS) {
-      const int side = ex_bias_side(p, k0, pmin, br.pos + (vt * 32 + 31) / p.Gp);
+      const int side = ex_bias_side(p, k0, pmin, br.pos + (vt * 32 + 31) / Gp);
       if (side != 0) {
         const float far = tl[side * p.D];
 #pragma unroll
@@ -166,10 +160,10 @@ __global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
       const float4 t = *reinterpret_cast<const float4*>(ys + (k * 32 + row) * YS + col);
       y.x += t.x * w, y.y += t.y * w, y.z += t.z * w, y.w += t.w * w;
     }
-    const int vr = vt * 32 + row, ir = vr / p.Gp, hr = hx * p.Gp + vr % p.Gp;
+    const int vr = vt * 32 + row, ir = vr / Gp, hr = hx * Gp + vr % Gp;
     if (ir >= br.qlen) L = 0.f;  // a padded query
     if (ir >= p.nq) continue;
-    if (p.splits > 1) {
+    if (splits > 1) {
       const int64_t R = ((int64_t)(split * p.B + b) * Hx + hx) * nvt * 32 + vr;
       *reinterpret_cast<float4*>(p.part_y + R * kDHead + col) = y;
       if ((threadIdx.x & 15) == 0) p.part_ml[R] = make_float2(M, L);
@@ -183,6 +177,18 @@ __global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
         p.lse[((int64_t)b * p.H + hr) * p.nq + ir] = L > 0.f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
     }
   }
+}
+
+template <typename T, bool BIAS, int ST>
+__global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
+  extern __shared__ __align__(16) char smem[];
+  const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp;
+  int bid = blockIdx.x;
+  const int vt = bid % nvt;
+  bid /= nvt;
+  const int hx = bid % Hx;
+  bid /= Hx;
+  ex_rows_block<T, BIAS, ST>(p, smem, vt, hx, bid % p.B, bid / p.B, p.splits, p.Gp);
 }
 
 // Joins the parts (at most 64) of a (query, head) row: a wave per row, a lane per part for the weights and per
@@ -227,7 +233,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_join(ExactParams p) {
 // correction of what has been summed, and keeps its relative precision, in bf16 too, up to the
 // type's range. A row whose sum passes 2^64 (logits 44 above M), or whose first keys the bias all
 // masked and whose sum is below 2^-20, has its block take the pass again with a running maximum.
-template <bool BIAS, int MT>
+template <bool BIAS, int MT, bool WIN>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 3 : 2))) void k_exact_tiles(ExactParams p) {
   constexpr int QB = 128 * MT;
   extern __shared__ __align__(16) char smem[];  // three K tiles, three V tiles, the bias table
@@ -235,13 +241,24 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
   const int c = lane & 31, hf = lane >> 5;
   int qt, pair;
   const int nqt = (p.nq + QB - 1) / QB;
-  ex_block_pair(blockIdx.x, nqt, p.H * p.B, p.causal || p.window, qt, pair);
+  int bid = blockIdx.x;
+  if constexpr (WIN) {  // the first blocks: the rows around a global query
+    if (bid < p.H * p.B) {
+      const int first = ex_global_rows(p, ex_batch_row(p, bid / p.H));
+      if (first >= 0) ex_rows_block<uint16_t, BIAS, 2>(p, smem, first / 32, bid % p.H, bid / p.H, 0, 1, 1);
+      return;
+    }
+    bid -= p.H * p.B;
+  }
+  ex_block_pair(bid, nqt, p.H * p.B, p.causal || p.window, qt, pair);
   if (p.causal) qt = nqt - 1 - qt;  // the longest rows first
   const int h = pair % p.H, b = pair / p.H, hk = h / p.G;
   const ExRow0 br = ex_batch_row(p, b);
   const int qw = qt * QB + wave * 32 * MT;  // the wave's first query
-  const int last = min(qt * QB + QB, br.qlen) - 1;
-  const ExTiles tiles = last >= qt * QB ? ex_key_tiles<64>(p, br.pos + qt * QB, br.pos + last, br.klen) : ExTiles{-1, 0, 0};
+  const int global = WIN ? ex_global_rows(p, br) : -1;
+  const int first = qt * QB + (WIN && global == qt * QB ? 32 : 0), last = min(qt * QB + QB, br.qlen) - 1;
+  const ExTiles tiles = last >= first ? ex_key_tiles<64>(p, br.pos + first, br.pos + last, br.klen, !WIN) : ExTiles{-1, 0, 0};
+  const bool mine = !WIN || qw != global;  // another block has the wave's rows
   // keys that all of the wave's queries attend
   const ExRange whole = ex_whole_keys(p, br.pos + qw, br.pos + min(qw + 32 * MT, br.qlen) - 1, br.klen);
 
@@ -412,12 +429,13 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     l[m] += ex_other_half(l[m]);
-    const bool live = qw + 32 * m + c < br.qlen && tiles.n > 0;
+    const bool live = qw + 32 * m + c < br.qlen && tiles.n > 0 && mine;
     again = again || (live && (!(l[m] <= 0x1p64f) || (BIAS && l[m] < 0x1p-20f)));
     if (!live) l[m] = 0.f;  // a padded query
   }
   // rows qw + 32 m on: their sums under -nmax, normalised and written
   auto store = [&](int m, float nmax, float sum, f32x16_t (&ym)[2]) __attribute__((always_inline)) {
+    if (!mine) return;
     const int first = qw + 32 * m, ln = ex_opaque(lane), i = first + (ln & 31);
     if (ln < 32 && i < p.nq) lse[i] = sum > 0.f ? (__builtin_amdgcn_logf(sum) - nmax) * kLn2 : -INFINITY;
     if (sum == 0.f) ym[0] = ym[1] = zero;  // what was summed for it may be anything
@@ -477,12 +495,17 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
   for (int m = 0; m < MT; ++m) store(m, nm[m], l[m], y[m]);
 }
 
-template <bool BIAS, int MT>
+template <bool BIAS, int MT, bool WIN>
 hipError_t launch_tiles(const ExactParams& p, hipStream_t s) {
-  const size_t lds = 6 * kTile64 + (BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0);
-  const int64_t blocks = (int64_t)((p.nq + 128 * MT - 1) / (128 * MT)) * p.H * p.B;
+  const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
+  const size_t lds = table + (WIN ? (size_t)kRowLds<uint16_t, 2> : 6 * kTile64);
+  const int64_t blocks = ((int64_t)((p.nq + 128 * MT - 1) / (128 * MT)) + WIN) * p.H * p.B;
+  if constexpr (WIN) {
+    const hipError_t e = exact_set_lds<k_exact_tiles<BIAS, MT, WIN>, 512>(lds);
+    if (e != hipSuccess) return e;
+  }
   static_assert(6 * kTile64 + (2 * kMaxBiasDistance + 129) * 4 <= 65536 - 512, "LDS that needs no leave");
-  hipLaunchKernelGGL((k_exact_tiles<BIAS, MT>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
+  hipLaunchKernelGGL((k_exact_tiles<BIAS, MT, WIN>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
   return hipGetLastError();
 }
 
@@ -552,8 +575,9 @@ int exact_splits(const ExactParams& p) {
 
 hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s) {
   if (forward_in_tiles(p)) {
-    if (p.table) return launch_tiles<true, 1>(p, s);
-    return forward_wide(p) ? launch_tiles<false, 2>(p, s) : launch_tiles<false, 1>(p, s);
+    if (p.window && !p.causal) return p.table ? launch_tiles<true, 1, true>(p, s) : launch_tiles<false, 1, true>(p, s);
+    if (p.table) return launch_tiles<true, 1, false>(p, s);
+    return forward_wide(p) ? launch_tiles<false, 2, false>(p, s) : launch_tiles<false, 1, false>(p, s);
   }
   if (p.bf16) return p.table ? launch_rows<uint16_t, true>(p, s) : launch_rows<uint16_t, false>(p, s);
   return p.table ? launch_rows<float, true>(p, s) : launch_rows<float, false>(p, s);
