@@ -972,6 +972,140 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   ex_store_rows32(st, dv, 1.f, out, p.dV.row * 2, p.nk - kw, lane);
 }
 
+// ------------------------------------------------------------------ up to 128 queries and keys, bf16
+// One launch for all three gradients: a block has a (batch row, head)'s Q, K, V and dY in LDS, its four waves
+// take 32 queries each for D and dQ, and then 32 keys each for dK and dV. What two launches cost at this size is
+// mostly their starts and loads (backward pass, 12 heads, two launches against one: 1 x 32 tokens 11.4 and 6.1
+// us; 1 x 128 11.8 and 10.4; 32 x 128 24.7 and 18.7; 128 x 128 69 and 51).
+constexpr int kSmallRows = 128;
+constexpr int kSmallLds = 4 * kSmallRows * 128 + 2 * kSmallRows * 4;  // the matrices, where S and dP start
+
+// 32 rows of a lane's own from registers: 8 bytes to a store (the LDS is all in use).
+__device__ __forceinline__ void ex_store_lane_row(const f32x16_t (&y)[2], float scale, uint16_t* row, int hf) {
+#pragma unroll
+  for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4)
+      *reinterpret_cast<uint2*>(row + 32 * cc + 2 * r + 4 * hf) =
+          make_uint2(pack_bf16x2(y[cc][r] * scale, y[cc][r + 1] * scale), pack_bf16x2(y[cc][r + 2] * scale, y[cc][r + 3] * scale));
+}
+
+__global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_backward_small(ExactParams p) {
+  using T = uint16_t;
+  extern __shared__ __align__(16) char smem[];  // Q, K, V, dY; -c / s2 and -D per query
+  char *Qs = smem, *Ks = smem + 16384, *Vs = smem + 32768, *Ys = smem + 49152;
+  float* stat = reinterpret_cast<float*>(smem + 65536);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, hf = lane >> 5, h = blockIdx.x % p.H, b = blockIdx.x / p.H, r0 = 32 * wave;
+  const ExRow0 br = ex_batch_row(p, b);
+  const int64_t hcol = h * kDHead;
+  const uint32_t to = lds_addr(smem) + 4096u * wave;
+  auto load = [&](const ExactRows& m, int limit, uint32_t at) __attribute__((always_inline)) {
+    const char* base = static_cast<const char*>(m.data) + (b * m.batch + hcol) * 2;
+    ex_load_tile<T>(ex_rsrc(base, m.row * 2, r0, limit, 128), (int)m.row * 2, to + at, lane);
+  };
+  load(p.K, br.klen, 16384);
+  load(p.V, br.klen, 32768);
+  load(p.Q, br.qlen, 0);
+  load(p.dY, br.qlen, 49152);
+  const int i = r0 + c;
+  float D = 0.f, cr = INFINITY;  // a row without keys, or behind the last query: every P is 0
+  if (i < br.qlen) {
+    const char* y = static_cast<const char*>(p.Y.data) + (b * p.Y.batch + i * p.Y.row + hcol) * 2;
+    const char* g = static_cast<const char*>(p.dY.data) + (b * p.dY.batch + i * p.dY.row + hcol) * 2;
+    D = ex_row_dot<T>(ex_global_row<T>(g, hf), ex_global_row<T>(y, hf), D);
+    const float lse = p.lse[((int64_t)b * p.H + h) * p.nq + i];
+    cr = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  }
+  D += ex_other_half(D);
+  wait_vmcnt<0>();
+  __syncthreads();
+
+  const int last = min(r0 + 32, br.qlen) - 1, pos = br.pos + i;
+  f32x16_t dq[2] = {ex_zero16(), ex_zero16()};
+  if (last >= r0) {  // wave-uniform
+    const ExTiles tiles = ex_key_tiles(p, br.pos + r0, br.pos + last, br.klen);
+    const ExSpan keys = ex_keys_of(p, pos, br.klen);
+    ExRow<T> q, dy;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      q.v[g] = ex_tile_chunk<T>(Qs + 4096 * wave, c, hf, g);
+      dy.v[g] = ex_tile_chunk<T>(Ys + 4096 * wave, c, hf, g);
+    }
+    f32x16_t pk[2] = {ex_zero16(), ex_zero16()};
+    float rest = 0.f;
+#pragma clang loop unroll(disable)
+    for (int t = 0; t < tiles.n; ++t) {
+      const int kt = ex_tile_at(tiles, t), k0 = 32 * kt;
+      f32x16_t x = ex_rows_product<T>(Ks + 4096 * kt, q, c, hf);
+      const f32x16_t dp = ex_rows_product<T>(Vs + 4096 * kt, dy, c, hf);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = __fmaf_rn(x[r], p.s2, -cr);
+      if (!ex_whole(p, br.pos + r0, br.pos + last, k0, br.klen)) ex_mask(x, keys, k0 + 4 * hf, k0 > 0);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = ex_exp2(x[r]);
+      ex_cols_product<T>(pk, Ks + 4096 * kt, x, lane);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] *= dp[r] - D;
+      rest += ex_sum16(x);
+      ex_cols_product<T>(dq, Ks + 4096 * kt, x, lane);
+    }
+    rest += ex_other_half(rest);  // the exact D less this one
+    D += rest;
+#pragma unroll
+    for (int cc = 0; cc < 2; ++cc)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq[cc][r] = fmaf(-rest, pk[cc][r], dq[cc][r]);
+  }
+  if (hf == 0) {
+    stat[i] = -cr * (1.f / p.s2);
+    stat[kSmallRows + i] = -D;
+  }
+  if (i < p.nq) ex_store_lane_row(dq, p.scale, static_cast<T*>(p.dQ.data) + b * p.dQ.batch + i * p.dQ.row + hcol, hf);
+  __syncthreads();
+
+  f32x16_t dk[2] = {ex_zero16(), ex_zero16()}, dv[2] = {ex_zero16(), ex_zero16()};
+  const int jmax = min(r0 + 32, br.klen) - 1;
+  if (jmax >= r0) {
+    const ExTiles tiles = ex_query_tiles(p, br, r0, jmax);
+    const ExSpan queries = ex_queries_of(p, br, r0 + c);
+    ExRow<T> kf, vf;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      kf.v[g] = ex_tile_chunk<T>(Ks + 4096 * wave, c, hf, g);
+      vf.v[g] = ex_tile_chunk<T>(Vs + 4096 * wave, c, hf, g);
+    }
+#pragma clang loop unroll(disable)
+    for (int t = 0; t < tiles.n; ++t) {
+      const int qt = ex_tile_at(tiles, t), i0 = 32 * qt, p0 = br.pos + i0;
+      f32x16_t x = ex_rows_product<T>(Qs + 4096 * qt, kf, c, hf);
+      f32x16_t ds = ex_rows_product<T>(Ys + 4096 * qt, vf, c, hf);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {  // rows 8 k + 4 hf ..
+        const float4 u = *reinterpret_cast<const float4*>(stat + i0 + 8 * k + 4 * hf);
+        const float4 w = *reinterpret_cast<const float4*>(stat + kSmallRows + i0 + 8 * k + 4 * hf);
+        x[4 * k] += u.x, x[4 * k + 1] += u.y, x[4 * k + 2] += u.z, x[4 * k + 3] += u.w;
+        ds[4 * k] += w.x, ds[4 * k + 1] += w.y, ds[4 * k + 2] += w.z, ds[4 * k + 3] += w.w;
+      }
+      if (i0 + 32 > br.qlen || !ex_whole(p, p0, p0 + 31, r0, 0x7fffffff)) ex_mask(x, queries, i0 + 4 * hf, p0 > 0);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[r] = ex_exp2(x[r] * p.s2);
+        ds[r] *= x[r];
+      }
+      ex_cols_product<T>(dv, Ys + 4096 * qt, x, lane);
+      ex_cols_product<T>(dk, Qs + 4096 * qt, ds, lane);
+    }
+  }
+  __syncthreads();
+  if (i >= br.klen) dk[0] = dk[1] = dv[0] = dv[1] = ex_zero16();
+  char* st = smem + wave * 32 * 144;
+  char* out = static_cast<char*>(p.dK.data) + (b * p.dK.batch + (int64_t)r0 * p.dK.row + hcol) * 2;
+  ex_store_rows32(st, dk, p.scale, out, p.dK.row * 2, p.nk - r0, lane);
+  out = static_cast<char*>(p.dV.data) + (b * p.dV.batch + (int64_t)r0 * p.dV.row + hcol) * 2;
+  ex_store_rows32(st, dv, 1.f, out, p.dV.row * 2, p.nk - r0, lane);
+}
+
 // Adds up what k_exact_dkv leaves in parts: the first `sums` blocks the bias gradient, one (bucket, head)
 // per wave; the others dK and dV, four columns of a key per thread.
 template <typename T>
@@ -1103,6 +1237,14 @@ hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
 
 template <typename T, bool BIAS>
 hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
+  if constexpr (ExFmt<T>::ES == 2 && !BIAS) {
+    if (p.nq <= kSmallRows && p.nk <= kSmallRows && p.G == 1) {
+      const hipError_t e = exact_set_lds<k_exact_backward_small>(kSmallLds);
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(k_exact_backward_small, dim3((unsigned)(p.H * p.B)), dim3(kExThreads), kSmallLds, s, p);
+      return hipGetLastError();
+    }
+  }
   const hipError_t e = launch_dq<T, BIAS>(p, s);
   return e != hipSuccess ? e : launch_dkv<T, BIAS>(p, s);
 }

@@ -66,6 +66,11 @@ SHAPES = [  # B, nq, nk, heads, kv_heads, options
     (2, 150, 150, 2, 2, dict(window=30, causal=True)),
     (2, 40, 200, 2, 2, dict(window=30, causal=True, q_pos=[-10, 100])),
     (1, 513, 511, 2, 1, {}),
+    # up to 128 queries and keys: one launch for the gradients in bfloat16
+    (3, 128, 100, 4, 4, dict(window=16, q_lens=[128, 33, 1], kv_lens=[100, 64, 2])),
+    (2, 100, 128, 3, 3, dict(window=30, causal=True, q_pos=[28, -40])),
+    (3, 127, 128, 5, 5, dict(causal=True, q_lens=[127, 96, 0], kv_lens=[128, 0, 65])),
+    (2, 65, 97, 4, 4, dict(window=6, q_pos=[-33, 20])),
     (2, 1057, 1057, 2, 2, dict(window=256, q_lens=[1057, 353], kv_lens=[1057, 353])),
     # more blocks of 32 rows than CUs: bfloat16 in blocks of 128 rows
     (9, 129, 127, 8, 8, {}),
