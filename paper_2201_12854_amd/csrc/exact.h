@@ -79,6 +79,7 @@ inline bool exact_worth(int64_t tiles, int64_t n, int unit) {
 }
 int exact_splits(const ExactParams& p);
 int exact_kv_splits(const ExactParams& p);
+bool exact_backward_small(const ExactParams& p);  // in one launch, without a workspace
 int64_t exact_bias_parts(const ExactParams& p);
 int exact_group(const ExactParams& p);  // Gp
 hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s);

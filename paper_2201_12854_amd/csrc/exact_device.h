@@ -455,6 +455,22 @@ __device__ __forceinline__ ExRange ex_whole_queries(const ExactParams& p, int j0
   if (p.window) r = ExRange{max(r.lo, j0 + 31 - p.half), min(r.hi, j0 + p.half - 31)};
   return r;
 }
+// Positions of the rows that attend more than one key, as far as lengths, causality and window say. In a row
+// outside P is 1 or 0 and dS is zero; its sums would leave their rounding instead, which is all there is of
+// a gradient where no row attends more (one token).
+__device__ __forceinline__ ExRange ex_many_keys(const ExactParams& p, int klen) {
+  if (klen < 2) return ExRange{1, 0};
+  ExRange r{p.causal ? 1 : -0x40000000, 0x40000000};
+  if (p.window) r = ExRange{max(r.lo, 1 - p.half), klen - 1 + p.half};
+  return r;
+}
+// Zeros dS of such rows in a half tile whose queries begin at position q0.
+__device__ __forceinline__ void ex_drop_single(f32x16_t& d, const ExRange& many, int q0, int hf) {
+  if (__builtin_expect(q0 < many.lo || q0 + 31 > many.hi, 0)) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) d[r] = ex_has(many, q0 + 4 * hf + (r & 3) + 8 * (r >> 2)) ? d[r] : 0.f;
+  }
+}
 
 // ------------------------------------------------------------------ relative bias
 // Bucket of the key rel = j - p places behind the query: distances below E have one each, distance

@@ -309,6 +309,7 @@ __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, in
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[cc][r] = fmaf(-rest, pk[cc][r], dq[cc][r]);
   }
+  if (!ex_has(ex_many_keys(p, br.klen), pos)) dq[0] = dq[1] = ex_zero16();
   ex_put_sums(ys, dq, wave * 32 + c, hf);
   if (wave == 0 && hf == 0 && i < p.nq) ex_put_stat<T>(p, ((int64_t)b * p.H + head) * p.nq + i, cr, D);
   __syncthreads();
@@ -346,6 +347,7 @@ __device__ __forceinline__ void ex_dkv_block(const ExactParams& p, char* smem, i
   const int j = kt * 32 + c, jmax = min(kt * 32 + 31, br.klen - 1);
   const ExTiles tiles = ex_query_tiles(p, br, kt * 32, jmax);
   const ExSpan queries = ex_queries_of(p, br, j);
+  const ExRange many = ex_many_keys(p, br.klen);
 
   const bool live = j < br.klen;
   const char* krow = static_cast<const char*>(p.K.data) + (b * p.K.batch + j * p.K.row + hk * kDHead) * ES;
@@ -413,6 +415,7 @@ __device__ __forceinline__ void ex_dkv_block(const ExactParams& p, char* smem, i
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] -= D[r];
       }
+      ex_drop_single(ds, many, p0, hf);
       int side = 0;
       if constexpr (BIAS) {
         for (const int h = idx / tiles.n; head < h; ++head) {
@@ -703,6 +706,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
     for (int r = 0; r < 16; ++r) dq[cc][r] = fmaf(-rest, pk[cc][r], dq[cc][r]);
+  if (!ex_has(ex_many_keys(p, br.klen), br.pos + i)) dq[0] = dq[1] = zero;
   wait_vmcnt<0>();  // no load is under way into what is written next
   __syncthreads();
   if (WIN && qw == global) return;  // another block has these rows
@@ -768,6 +772,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   };
   const bool mine = !WIN || kw > 0;  // another block has the first 32 keys
   const ExRange whole = ex_whole_queries(p, kw, !mine ? 0 : BIAS ? br.klen : 0x7fffffff);
+  const ExRange many = ex_many_keys(p, br.klen);
   float fac = p.s2, add = 0.f, far_l = 0.f, far_r = 0.f;
   int side = 0, entry = 0;  // where the half tile lies, and the entry of its first key and query
   const float* tl = nullptr;
@@ -786,8 +791,9 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       for (int r = 0; r < 16; ++r) bv[r] = at[-((r & 3) + 8 * (r >> 2))];
     }
   };
-  auto fix = [&](f32x16_t& s, int i0) __attribute__((always_inline)) {
+  auto fix = [&](f32x16_t& s, f32x16_t& d, int i0) __attribute__((always_inline)) {
     const int q0 = br.pos + i0;
+    ex_drop_single(d, many, q0, hf);
     if constexpr (BIAS) {
       side = next;
       entry = p.D + 64 + kw - q0;
@@ -922,9 +928,9 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
       const char *ct = smem + b0 * kDkvTilesStage, *nt = smem + b1 * kDkvTilesStage;
       const bool last = t + 1 == tiles.n;  // the next tile is the next head's first
       const int i0 = ex_tile_at(tiles, t) * 64, in = ex_tile_at(tiles, last ? 0 : t + 1) * 64;
-      fix(s0, i0);
+      fix(s0, p0, i0);
       step(s0, p0, s1, p1, ct, 0, ct, 1, nt, 0, i0 + 32, tl);
-      fix(s1, i0 + 32);
+      fix(s1, p1, i0 + 32);
       step(s1, p1, s0, p0, ct, 1, nt, 0, nt, 1, in, last && g + 1 < ng ? tl + n : tl);
       const int o = b0;
       b0 = b1;
@@ -1022,6 +1028,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   __syncthreads();
 
   const int last = min(r0 + 32, br.qlen) - 1, pos = br.pos + i;
+  const ExRange many = ex_many_keys(p, br.klen);
   f32x16_t dq[2] = {ex_zero16(), ex_zero16()};
   if (last >= r0) {  // wave-uniform
     const ExTiles tiles = ex_key_tiles(p, br.pos + r0, br.pos + last, br.klen);
@@ -1056,6 +1063,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[cc][r] = fmaf(-rest, pk[cc][r], dq[cc][r]);
+    if (!ex_has(many, pos)) dq[0] = dq[1] = ex_zero16();
   }
   if (hf == 0) {
     stat[i] = -cr * (1.f / p.s2);
@@ -1087,6 +1095,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
         x[4 * k] += u.x, x[4 * k + 1] += u.y, x[4 * k + 2] += u.z, x[4 * k + 3] += u.w;
         ds[4 * k] += w.x, ds[4 * k + 1] += w.y, ds[4 * k + 2] += w.z, ds[4 * k + 3] += w.w;
       }
+      ex_drop_single(ds, many, p0, hf);
       if (i0 + 32 > br.qlen || !ex_whole(p, p0, p0 + 31, r0, 0x7fffffff)) ex_mask(x, queries, i0 + 4 * hf, p0 > 0);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -1238,7 +1247,7 @@ hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
 template <typename T, bool BIAS>
 hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
   if constexpr (ExFmt<T>::ES == 2 && !BIAS) {
-    if (p.nq <= kSmallRows && p.nk <= kSmallRows && p.G == 1) {
+    if (exact_backward_small(p)) {
       const hipError_t e = exact_set_lds<k_exact_backward_small>(kSmallLds);
       if (e != hipSuccess) return e;
       hipLaunchKernelGGL(k_exact_backward_small, dim3((unsigned)(p.H * p.B)), dim3(kExThreads), kSmallLds, s, p);
@@ -1251,12 +1260,16 @@ hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
 
 }  // namespace
 
+bool exact_backward_small(const ExactParams& p) {
+  return p.bf16 && !p.table && p.nq <= kSmallRows && p.nk <= kSmallRows && p.G == 1;
+}
+
 // Blocks that share a key's queries: where they leave CUs without one (few keys, or few key heads with
 // many query heads), as many as that takes, of sixteen tiles of 64 at least, or a tile of 32 to a wave
 // where that saves more than the join takes.
 int exact_kv_splits(const ExactParams& p) {
   const bool big = dkv_in_tiles(p);
-  if (big && p.window) return 1;
+  if ((big && p.window) || exact_backward_small(p)) return 1;
   const int64_t blocks = (int64_t)((p.nk + (big ? 127 : 31)) / (big ? 128 : 32)) * p.Hk * p.B;
   const int64_t tiles = (int64_t)p.G * ((p.nq + (big ? 63 : 31)) / (big ? 64 : 32));
   const int64_t n = std::min((big ? 2 : 1) * device_cus() / blocks, tiles / (big ? 16 : kExWaves));

@@ -126,6 +126,42 @@ def test_relative_bias(dtype, shape):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,nq,nk,heads,kv,opt", [
+    (1, 1, 1, 2, 2, {}),
+    (2, 1, 1, 8, 2, dict(buckets=8)),
+    (64, 1, 1, 12, 12, dict(buckets=32)),  # in bfloat16, blocks of 128 rows
+    (64, 1, 1, 12, 3, {}),
+    (3, 200, 130, 4, 4, dict(kv_lens=[1, 130, 0])),
+    (4, 1, 300, 4, 2, dict(causal=True, buckets=8, bidirectional=False, q_pos=[0, 0, -3, 5])),
+    (20, 300, 300, 8, 8, dict(causal=True)),
+    (4, 40, 70, 3, 3, dict(window=10, q_pos=[-60, 75, 70, -20])),
+    (80, 40, 70, 4, 4, dict(window=10, buckets=8, q_pos=[-60, 75, 70, -20] * 20)),
+])
+def test_rows_with_one_key(dtype, B, nq, nk, heads, kv, opt):
+    """A row that attends one key has no gradient but dV's, and leaves no rounding in the others."""
+    t, kw, bias = _make(dtype, B, nq, nk, heads, kv, **opt)
+    print(f"[case] one key {dtype} {B} {nq} {nk} {heads} {kv} {opt}", flush=True)
+    got = _check(t, kw, bias)
+    i, j = torch.arange(nq, device=DEV), torch.arange(nk, device=DEV)
+    pos = i[None] + (0 if kw["q_pos"] is None else kw["q_pos"][:, None])
+    rel = j[None, None] - pos[:, :, None]
+    ok = torch.ones(B, nq, nk, dtype=torch.bool, device=DEV)
+    if kw["kv_lens"] is not None:
+        ok &= (j[None] < kw["kv_lens"][:, None])[:, None]
+    if kw["causal"]:
+        ok &= rel <= 0
+    if kw["window"]:
+        ok &= (rel.abs() <= kw["window"] // 2) | (pos == 0)[:, :, None] | (j == 0)[None, None]
+    one = ok.sum(-1) <= 1
+    assert one.any()
+    assert (got["dQ"][one] == 0).all()
+    still = ~(ok & ~one[:, :, None]).any(1)  # keys that no other row attends
+    assert (got["dK"][still] == 0).all()
+    if one.all() and "dbias" in got:
+        assert (got["dbias"] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("low", [float("-inf"), -1e30, "lowest"])
 @pytest.mark.parametrize("B,heads", [(2, 3), (14, 5)])  # blocks of 32 and, in bfloat16, of 128 rows
 def test_bias_that_masks(dtype, low, B, heads):
