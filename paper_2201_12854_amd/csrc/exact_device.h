@@ -141,16 +141,19 @@ __device__ __forceinline__ f32x16_t ex_rows_product(const char* tile, const ExRo
 }
 
 // y[cc] += tile^T x over the tile's 32 rows: rows of y are columns 32 cc .. 32 cc + 31 of the
-// tile. In bf16 x is rounded to bf16 for the product: half the matrix instruction's precision is
-// the type's own.
-template <typename T>
+// tile. In bf16 x is rounded to bf16 for the product, half a step of the result's own type; FINE: what the
+// rounding took off is multiplied too, in products of its own. (Sums of few terms take that: the roundings of many
+// average out, and bring a result's error in norm from the 1.66e-3 of its own rounding to 2.4e-3, those of
+// a few of nearly equal size, as two keys have them, to 2.9e-3. For all rows it would cost the forward pass
+// 0.3 to 0.7 us of 8, the backward pass 3 to 12%.)
+template <typename T, bool FINE = false>
 __device__ __forceinline__ void ex_cols_product(f32x16_t (&y)[2], const char* tile, const f32x16_t& x, int lane) {
   const int hf = lane >> 5;
   if constexpr (ExFmt<T>::ES == 2) {
     const int i16 = lane & 15, r0 = 4 * hf + (i16 >> 2);
 #pragma unroll
     for (int pp = 0; pp < 2; ++pp) {
-      u32x4_t b;
+      u32x4_t b, t[2];
 #pragma unroll
       for (int w = 0; w < 4; ++w) b[w] = pack_bf16x2(x[8 * pp + 2 * w], x[8 * pp + 2 * w + 1]);
 #pragma unroll
@@ -165,7 +168,16 @@ __device__ __forceinline__ void ex_cols_product(f32x16_t (&y)[2], const char* ti
           const char* at = tile + row * 128 + (((col >> 3) ^ ex_swz<T>(row)) << 4) + (col & 7) * 2;
           h[k] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)at));
         }
-        y[cc] = ex_mfma<T>(u32x4_t{h[0].x, h[0].y, h[1].x, h[1].y}, b, y[cc]);
+        t[cc] = u32x4_t{h[0].x, h[0].y, h[1].x, h[1].y};
+        y[cc] = ex_mfma<T>(t[cc], b, y[cc]);
+      }
+      if constexpr (FINE) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          b[w] = pack_bf16x2(x[8 * pp + 2 * w] - __uint_as_float(b[w] << 16),
+                             x[8 * pp + 2 * w + 1] - __uint_as_float(b[w] & 0xffff0000u));
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc) y[cc] = ex_mfma<T>(t[cc], b, y[cc]);
       }
     }
   } else {

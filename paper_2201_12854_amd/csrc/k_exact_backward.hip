@@ -189,6 +189,10 @@ __device__ __forceinline__ float ex_row_dot(const ExRow<T>& a, const ExRow<T>& b
   return D;
 }
 
+// FEW of the kernels below: P and dS are multiplied to more than the type's bits (ex_cols_product). For calls
+// of few pairs: up to 32 queries or keys, a tile, where it takes less than 0.5 us.
+bool few(const ExactParams& p) { return p.bf16 && std::min(p.nq, p.nk) <= 32; }
+
 // ------------------------------------------------------------------ dQ
 // Blocks of 32 (query, head) rows whose key tiles the waves share, as k_exact_rows. S^T = K Q^T
 // and dP^T = V dY^T: the row's c and D are one value per lane, and dS feeds dQ^T = K^T dS^T.
@@ -202,7 +206,7 @@ __device__ __forceinline__ float ex_row_dot(const ExRow<T>& a, const ExRow<T>& b
 // comes from large P, and is multiplied by them: the kernel of 64-row tiles leaves half tiles out of sum_j P k
 // whose P are all at most kSmallP (at 4 x 4096 tokens, 12 heads, all of them: dQ 317 us without this, 427
 // with every tile's product).
-template <typename T, bool BIAS, int ST>
+template <typename T, bool BIAS, int ST, bool FEW>
 __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, int vt, int hx, int b, int Gp) {
   constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>();
   const int n = 2 * p.D + 129;
@@ -288,7 +292,7 @@ __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, in
     if constexpr (ES == 2) ex_cols_product<T>(pk, kt, x, lane);
 #pragma unroll
     for (int r = 0; r < 16; ++r) x[r] *= dp[r] - D;
-    ex_cols_product<T>(dq, kt, x, lane);
+    ex_cols_product<T, FEW>(dq, kt, x, lane);
     if constexpr (ES == 2) rest += ex_sum16(x);
     slot = slot == ST - 1 ? 0 : slot + 1;
   }
@@ -323,11 +327,11 @@ __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, in
   }
 }
 
-template <typename T, bool BIAS, int ST>
+template <typename T, bool BIAS, int ST, bool FEW = false>
 __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
   extern __shared__ __align__(16) char smem[];
   const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp, bid = blockIdx.x / nvt;
-  ex_dq_block<T, BIAS, ST>(p, smem, blockIdx.x % nvt, bid % Hx, bid / Hx, p.Gp);
+  ex_dq_block<T, BIAS, ST, FEW>(p, smem, blockIdx.x % nvt, bid % Hx, bid / Hx, p.Gp);
 }
 
 // ------------------------------------------------------------------ dK, dV
@@ -335,7 +339,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
 // block's part of them (kv_splits). S = Q K^T and dP = dY V^T with the lane holding a key: P and dS
 // feed dV^T = dY^T P and dK^T = Q^T dS. A wave loads its tiles of Q, dY and row statistics straight
 // into LDS.
-template <typename T, bool BIAS, int ST>
+template <typename T, bool BIAS, int ST, bool FEW>
 __device__ __forceinline__ void ex_dkv_block(const ExactParams& p, char* smem, int kt, int hk, int b, int split, int splits,
                                              int64_t part, int heads_at_once) {
   constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>(), SB = kDkvStage<T>;
@@ -446,8 +450,8 @@ __device__ __forceinline__ void ex_dkv_block(const ExactParams& p, char* smem, i
         x[r] = ex_exp2(x[r]);
         ds[r] *= x[r];
       }
-      ex_cols_product<T>(dv, qt + TB, x, lane);
-      ex_cols_product<T>(dk, qt, ds, lane);
+      ex_cols_product<T, FEW>(dv, qt + TB, x, lane);
+      ex_cols_product<T, FEW>(dk, qt, ds, lane);
       if constexpr (BIAS) {
         if (side < 0) far_l += ex_sum16(ds);
         else if (side > 0) far_r += ex_sum16(ds);
@@ -486,7 +490,7 @@ __device__ __forceinline__ void ex_dkv_block(const ExactParams& p, char* smem, i
   }
 }
 
-template <typename T, bool BIAS, int ST>
+template <typename T, bool BIAS, int ST, bool FEW = false>
 __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int heads_at_once) {
   extern __shared__ __align__(16) char smem[];
   const int nkt = (p.nk + 31) / 32;
@@ -496,7 +500,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
   const int hk = bid % p.Hk;
   bid /= p.Hk;
   const int64_t part = ((int64_t)bid * nkt + kt) * kExWaves;  // bid: split * B + batch row
-  ex_dkv_block<T, BIAS, ST>(p, smem, kt, hk, bid % p.B, bid / p.B, p.kv_splits, part, heads_at_once);
+  ex_dkv_block<T, BIAS, ST, FEW>(p, smem, kt, hk, bid % p.B, bid / p.B, p.kv_splits, part, heads_at_once);
 }
 
 // ------------------------------------------------------------------ tiles of 64 rows, bf16
@@ -539,7 +543,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   if constexpr (WIN) {  // the first blocks: the rows around a global query
     if (bid < p.H * p.B) {
       const int first = ex_global_rows(p, ex_batch_row(p, bid / p.H));
-      if (first >= 0) ex_dq_block<uint16_t, BIAS, 2>(p, smem, first / 32, bid % p.H, bid / p.H, 1);
+      if (first >= 0) ex_dq_block<uint16_t, BIAS, 2, false>(p, smem, first / 32, bid % p.H, bid / p.H, 1);
       return;
     }
     bid -= p.H * p.B;
@@ -731,7 +735,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   if constexpr (WIN) {  // the first blocks: the keys around the global one (kv_splits is 1)
     if (bid < p.Hk * p.B) {
       const int64_t part = ((int64_t)p.B * nkt + bid / p.Hk) * kExWaves;
-      ex_dkv_block<uint16_t, BIAS, 2>(p, smem, 0, bid % p.Hk, bid / p.Hk, 0, 1, part, heads_at_once);
+      ex_dkv_block<uint16_t, BIAS, 2, false>(p, smem, 0, bid % p.Hk, bid / p.Hk, 0, 1, part, heads_at_once);
       return;
     }
     bid -= p.Hk * p.B;
@@ -996,6 +1000,7 @@ __device__ __forceinline__ void ex_store_lane_row(const f32x16_t (&y)[2], float 
           make_uint2(pack_bf16x2(y[cc][r] * scale, y[cc][r + 1] * scale), pack_bf16x2(y[cc][r + 2] * scale, y[cc][r + 3] * scale));
 }
 
+template <bool FEW>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_backward_small(ExactParams p) {
   using T = uint16_t;
   extern __shared__ __align__(16) char smem[];  // Q, K, V, dY; -c / s2 and -D per query
@@ -1055,7 +1060,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
 #pragma unroll
       for (int r = 0; r < 16; ++r) x[r] *= dp[r] - D;
       rest += ex_sum16(x);
-      ex_cols_product<T>(dq, Ks + 4096 * kt, x, lane);
+      ex_cols_product<T, FEW>(dq, Ks + 4096 * kt, x, lane);
     }
     rest += ex_other_half(rest);  // the exact D less this one
     D += rest;
@@ -1102,8 +1107,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
         x[r] = ex_exp2(x[r] * p.s2);
         ds[r] *= x[r];
       }
-      ex_cols_product<T>(dv, Ys + 4096 * qt, x, lane);
-      ex_cols_product<T>(dk, Qs + 4096 * qt, ds, lane);
+      ex_cols_product<T, FEW>(dv, Ys + 4096 * qt, x, lane);
+      ex_cols_product<T, FEW>(dk, Qs + 4096 * qt, ds, lane);
     }
   }
   __syncthreads();
@@ -1193,16 +1198,17 @@ hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
   }
   const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
   const size_t one = kDqLds<T, 1> + table * p.Gp, two = kDqLds<T, 2> + table * p.Gp;
+  auto launch = [&](auto kernel, hipError_t set, size_t lds) {
+    if (set != hipSuccess) return set;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
+    return hipGetLastError();
+  };
   if constexpr (ExFmt<T>::ES == 4) {  // as the forward pass
-    if (blocks > device_cus()) {
-      if ((e = exact_set_lds<k_exact_dq<T, BIAS, 1>>(one)) != hipSuccess) return e;
-      hipLaunchKernelGGL((k_exact_dq<T, BIAS, 1>), dim3((unsigned)blocks), dim3(kExThreads), one, s, p);
-      return hipGetLastError();
-    }
+    if (blocks > device_cus()) return launch(k_exact_dq<T, BIAS, 1>, exact_set_lds<k_exact_dq<T, BIAS, 1>>(one), one);
+  } else {
+    if (few(p)) return launch(k_exact_dq<T, BIAS, 2, true>, exact_set_lds<k_exact_dq<T, BIAS, 2, true>>(two), two);
   }
-  if ((e = exact_set_lds<k_exact_dq<T, BIAS, 2>>(two)) != hipSuccess) return e;
-  hipLaunchKernelGGL((k_exact_dq<T, BIAS, 2>), dim3((unsigned)blocks), dim3(kExThreads), two, s, p);
-  return hipGetLastError();
+  return launch(k_exact_dq<T, BIAS, 2>, exact_set_lds<k_exact_dq<T, BIAS, 2>>(two), two);
 }
 
 // A block's tiles and its waves' sums along diagonals in LDS, then the bias tables of as many heads as fit.
@@ -1231,6 +1237,8 @@ hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
     if constexpr (ExFmt<T>::ES == 4)  // (as the forward pass)
       if ((int64_t)((p.nk + 31) / 32) * p.Hk * p.B * p.kv_splits > device_cus())
         e = launch_dkv_kernel<k_exact_dkv<T, BIAS, 1>, BIAS>(p, 32, kDkvLds<T, 1>, s);
+    if constexpr (ExFmt<T>::ES == 2)
+      if (few(p)) e = launch_dkv_kernel<k_exact_dkv<T, BIAS, 2, true>, BIAS>(p, 32, kDkvLds<T, 2>, s);
     if (e == hipErrorNotReady) e = launch_dkv_kernel<k_exact_dkv<T, BIAS, 2>, BIAS>(p, 32, kDkvLds<T, 2>, s);
   } else if constexpr (ExFmt<T>::ES == 2) {
     if (p.window) e = launch_dkv_kernel<k_exact_dkv_tiles<BIAS, true>, BIAS>(p, 128, kDkvLds<T, 2>, s, p.Hk * p.B);
@@ -1248,9 +1256,11 @@ template <typename T, bool BIAS>
 hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
   if constexpr (ExFmt<T>::ES == 2 && !BIAS) {
     if (exact_backward_small(p)) {
-      const hipError_t e = exact_set_lds<k_exact_backward_small>(kSmallLds);
+      const bool f = few(p);
+      const hipError_t e = f ? exact_set_lds<k_exact_backward_small<true>>(kSmallLds) : exact_set_lds<k_exact_backward_small<false>>(kSmallLds);
       if (e != hipSuccess) return e;
-      hipLaunchKernelGGL(k_exact_backward_small, dim3((unsigned)(p.H * p.B)), dim3(kExThreads), kSmallLds, s, p);
+      hipLaunchKernelGGL(f ? k_exact_backward_small<true> : k_exact_backward_small<false>, dim3((unsigned)(p.H * p.B)),
+                         dim3(kExThreads), kSmallLds, s, p);
       return hipGetLastError();
     }
   }

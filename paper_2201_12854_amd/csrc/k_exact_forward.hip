@@ -52,7 +52,7 @@ __device__ __forceinline__ void ex_softmax_step(ExState& s, f32x16_t& x) {
 template <typename T, int ST> constexpr int kRowLds = kExWaves * ST * 2 * tile_bytes<T>();
 
 // ST: tiles in LDS per wave, all but one of them on their way.
-template <typename T, bool BIAS, int ST>
+template <typename T, bool BIAS, int ST, bool FEW>
 __device__ __forceinline__ void ex_rows_block(const ExactParams& p, char* smem, int vt, int hx, int b, int split, int splits,
                                               int Gp) {
   constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>();
@@ -126,7 +126,7 @@ __device__ __forceinline__ void ex_rows_block(const ExactParams& p, char* smem, 
       ex_mask(x, keys, k0 + 4 * hf, k0 > 0);
     }
     ex_softmax_step(s, x);
-    ex_cols_product<T>(s.y, kt + TB, x, lane);
+    ex_cols_product<T, FEW>(s.y, kt + TB, x, lane);
     slot = slot == ST - 1 ? 0 : slot + 1;
   }
   s.l += ex_other_half(s.l);
@@ -179,7 +179,7 @@ __device__ __forceinline__ void ex_rows_block(const ExactParams& p, char* smem, 
   }
 }
 
-template <typename T, bool BIAS, int ST>
+template <typename T, bool BIAS, int ST, bool FEW>
 __global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
   extern __shared__ __align__(16) char smem[];
   const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp;
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
   bid /= nvt;
   const int hx = bid % Hx;
   bid /= Hx;
-  ex_rows_block<T, BIAS, ST>(p, smem, vt, hx, bid % p.B, bid / p.B, p.splits, p.Gp);
+  ex_rows_block<T, BIAS, ST, FEW>(p, smem, vt, hx, bid % p.B, bid / p.B, p.splits, p.Gp);
 }
 
 // Joins the parts (at most 64) of a (query, head) row: a wave per row, a lane per part for the weights and per
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
   if constexpr (WIN) {  // the first blocks: the rows around a global query
     if (bid < p.H * p.B) {
       const int first = ex_global_rows(p, ex_batch_row(p, bid / p.H));
-      if (first >= 0) ex_rows_block<uint16_t, BIAS, 2>(p, smem, first / 32, bid % p.H, bid / p.H, 0, 1, 1);
+      if (first >= 0) ex_rows_block<uint16_t, BIAS, 2, false>(p, smem, first / 32, bid % p.H, bid / p.H, 0, 1, 1);
       return;
     }
     bid -= p.H * p.B;
@@ -509,17 +509,21 @@ hipError_t launch_tiles(const ExactParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, bool BIAS, int ST>
+template <typename T, bool BIAS, int ST, bool FEW = false>
 hipError_t launch_rows_of(const ExactParams& p, hipStream_t s) {
   const size_t lds = kRowLds<T, ST> + (BIAS ? (size_t)p.Gp * exact_bias_entries(p.D) * 4 : 0);
-  hipError_t e = exact_set_lds<k_exact_rows<T, BIAS, ST>>(lds);
+  hipError_t e = exact_set_lds<k_exact_rows<T, BIAS, ST, FEW>>(lds);
   if (e != hipSuccess) return e;
   const int64_t rows = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
-  hipLaunchKernelGGL((k_exact_rows<T, BIAS, ST>), dim3((unsigned)(rows * p.splits)), dim3(kExThreads), lds, s, p);
+  hipLaunchKernelGGL((k_exact_rows<T, BIAS, ST, FEW>), dim3((unsigned)(rows * p.splits)), dim3(kExThreads), lds, s, p);
   if ((e = hipGetLastError()) != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL((k_exact_join<T>), dim3((unsigned)(((int64_t)p.B * p.H * p.nq + kExWaves - 1) / kExWaves)), dim3(kExThreads), 0, s, p);
   return hipGetLastError();
 }
+
+// FEW: P is multiplied to more than the type's bits (ex_cols_product). Up to these many keys, a tile to each
+// wave.
+constexpr int kFewKeys = 128;
 
 // bf16: two tiles, 64 KB of LDS for a block, two of them to a CU. float32, whose tiles are twice as large: two
 // where every block has a CU of its own, else one and two blocks to a CU, which cover each other's loads
@@ -528,6 +532,8 @@ template <typename T, bool BIAS>
 hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
   if constexpr (ExFmt<T>::ES == 4)
     if (exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B * p.splits > device_cus()) return launch_rows_of<T, BIAS, 1>(p, s);
+  if constexpr (ExFmt<T>::ES == 2)
+    if (p.nk <= kFewKeys) return launch_rows_of<T, BIAS, 2, true>(p, s);
   return launch_rows_of<T, BIAS, 2>(p, s);
 }
 
