@@ -253,7 +253,8 @@ mca_status mca_attention_forward_noalloc(const mca_forward_desc* desc, const voi
  *   (the sums of dk and dv run over the H / H_k query heads of the key head too)
  *   dbias_table[c, h] = sum of dS_ij over the pairs of head h in bucket c, all batch rows
  * Logits, softmax statistics and all sums are float32; with bfloat16 inputs P and dS enter
- * their matrix products rounded to bfloat16, and results are rounded once.
+ * their matrix products rounded to bfloat16 (to twice the bits in calls of few keys or
+ * queries), and results are rounded once.
  * Q, K, V, dY and the bias are expected to be finite (the bias: or masking); a non-finite
  * value in an attended row makes results that depend on it unspecified.
  *
@@ -308,7 +309,8 @@ mca_status mca_exact_workspace_size(const mca_exact_desc* desc, int backward, si
  * Y and lse of exact attention. `workspace` may be NULL when its size is 0; its contents on
  * entry do not matter. Errors: MCA_ERR_INVALID_ARGUMENT (null pointer, size < 1, kv_heads
  * that does not divide heads, bad scale, window, bias sizes, strides or alignment, reserved
- * not 0, a problem too large for one launch), MCA_ERR_UNSUPPORTED (d_head != 64),
+ * not 0, a result that begins where an operand or another result does, a problem too large
+ * for one launch), MCA_ERR_UNSUPPORTED (d_head != 64),
  * MCA_ERR_WORKSPACE_TOO_SMALL, MCA_ERR_HIP.
  */
 mca_status mca_exact_attention_forward(const mca_exact_desc* desc, const mca_rows* Q, const mca_rows* K,

@@ -391,14 +391,19 @@ class RelativeBias:
     bidirectional: bool = True
 
 
+def _int32(name, v) -> int:
+    if not -2**31 <= int(v) < 2**31:  # ctypes would take it modulo 2^32
+        raise ValueError(f"{name} must be a 32-bit integer (got {v})")
+    return int(v)
+
+
 def relative_buckets(buckets: int, max_distance: int = 128, bidirectional: bool = True) -> list:
     """The bucket of every relative position -max_distance .. max_distance (further ones share the
     end's), as a list of 2 max_distance + 1 integers."""
-    n = 2 * int(max_distance) + 1
-    out = (ctypes.c_int32 * max(n, 1))()
-    _check(load_library().mca_relative_buckets(int(buckets), int(max_distance), int(bool(bidirectional)), out),
-           "mca_relative_buckets")
-    return list(out)
+    out = (ctypes.c_int32 * 513)()  # of the largest max_distance, 256
+    _check(load_library().mca_relative_buckets(_int32("buckets", buckets), _int32("max_distance", max_distance),
+                                               int(bool(bidirectional)), out), "mca_relative_buckets")
+    return list(out[:2 * int(max_distance) + 1])
 
 
 @dataclass
@@ -453,7 +458,7 @@ class _ExactCall:
             if t.dim() != 2 or t.shape[1] != heads or t.dtype != dtype or t.device != dev or not t.is_contiguous():
                 raise ValueError(f"bias.table must be a contiguous {dtype} [buckets, {heads}] on {dev}")
             d.bias_table, d.bias_buckets = t.data_ptr(), t.shape[0]
-            d.bias_max_distance, d.bias_bidirectional = int(bias.max_distance), int(bool(bias.bidirectional))
+            d.bias_max_distance, d.bias_bidirectional = _int32("bias.max_distance", bias.max_distance), int(bool(bias.bidirectional))
         self._keep = (Q, K, V, q_lens, kv_lens, q_pos, bias)
 
     def rows(self, name, t, shape) -> Rows:

@@ -1,6 +1,7 @@
 // C ABI of exact attention: argument checks, the buckets' borders, workspace layout, launches.
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "exact.h"
 #include "mca_kernels.h"
@@ -189,6 +190,18 @@ mca_status check_workspace(const void* ws, size_t bytes, size_t need) {
   return MCA_OK;
 }
 
+// Results that begin where another operand does: in-place calls, one buffer for two gradients. (Overlaps in general
+// are not looked for: gradients may be interleaved slices of one tensor.)
+mca_status check_apart(std::initializer_list<const void*> in, std::initializer_list<const void*> out) {
+  for (const void* const* o = out.begin(); o != out.end(); ++o) {
+    for (const void* x : in)
+      if (*o && x == *o) return fail(MCA_ERR_INVALID_ARGUMENT, "a result must not be in an operand's memory");
+    for (const void* const* u = out.begin(); u != o; ++u)
+      if (*o && *u == *o) return fail(MCA_ERR_INVALID_ARGUMENT, "two results must not be in the same memory");
+  }
+  return MCA_OK;
+}
+
 mca::ExactRows rows_in(const mca_rows* t) { return {t->data, t->batch_stride, t->row_stride}; }
 mca::ExactOut rows_out(const mca_rows* t) { return {t->data, t->batch_stride, t->row_stride}; }
 
@@ -237,6 +250,7 @@ mca_status mca_exact_attention_forward(const mca_exact_desc* desc, const mca_row
   if (!lse || !aligned16(lse)) return fail(MCA_ERR_INVALID_ARGUMENT, "lse must be a 16-byte aligned device pointer");
   ExactParams p = params_of(*desc, false);
   if ((st = check_workspace(workspace, workspace_bytes, carve(p, false, static_cast<char*>(workspace)))) != MCA_OK) return st;
+  if ((st = check_apart({Q->data, K->data, V->data, desc->bias_table}, {Y->data, lse, workspace})) != MCA_OK) return st;
   p.Q = rows_in(Q);
   p.K = rows_in(K);
   p.V = rows_in(V);
@@ -269,6 +283,8 @@ mca_status mca_exact_attention_backward(const mca_exact_desc* desc, const mca_ro
   if (!aligned16(dbias_table)) return fail(MCA_ERR_INVALID_ARGUMENT, "device pointers must be 16-byte aligned");
   ExactParams p = params_of(*desc, true);
   if ((st = check_workspace(workspace, workspace_bytes, carve(p, true, static_cast<char*>(workspace)))) != MCA_OK) return st;
+  if ((st = check_apart({dY->data, Q->data, K->data, V->data, Y->data, lse, desc->bias_table},
+                        {dQ->data, dK->data, dV->data, dbias_table, workspace})) != MCA_OK) return st;
   p.Q = rows_in(Q);
   p.K = rows_in(K);
   p.V = rows_in(V);

@@ -100,13 +100,13 @@ def _rows(data=FAKE, batch=1 << 20, row=1024):
 
 
 def _forward(d, lse=FAKE, ws=None, ws_bytes=0, **rows):
-    t = dict(Q=_rows(), K=_rows(), V=_rows(), Y=_rows())
+    t = {n: _rows(FAKE + (k + 1 << 44)) for k, n in enumerate(("Q", "K", "V", "Y"))}
     t.update(rows)
     return mca.load_library().mca_exact_attention_forward(d, t["Q"], t["K"], t["V"], t["Y"], lse, ws, ws_bytes, None)
 
 
-def _backward(d, lse=FAKE, dbias=None, ws=FAKE, ws_bytes=1 << 40, **rows):
-    t = {n: _rows() for n in ("dY", "Q", "K", "V", "Y", "dQ", "dK", "dV")}
+def _backward(d, lse=FAKE, dbias=None, ws=FAKE + (1 << 43), ws_bytes=1 << 40, **rows):
+    t = {n: _rows(FAKE + (k + 1 << 44)) for k, n in enumerate(("dY", "Q", "K", "V", "Y", "dQ", "dK", "dV"))}
     t.update(rows)
     return mca.load_library().mca_exact_attention_backward(d, t["dY"], t["Q"], t["K"], t["V"], t["Y"], lse, t["dQ"], t["dK"],
                                                            t["dV"], dbias, ws, ws_bytes, None)
@@ -131,6 +131,29 @@ def test_overlapping_outputs_refused():
         assert _backward(_desc(), **{name: once}) == binding.MCA_ERR_INVALID_ARGUMENT, name
         # half of the rows of the next batch row
         assert _backward(_desc(), **{name: _rows(batch=1024 * 64)}) == binding.MCA_ERR_INVALID_ARGUMENT, name
+
+
+def test_results_in_place_refused():
+    at = lambda k: _rows(FAKE + (k << 44))  # noqa: E731
+    said = lambda: mca.load_library().mca_last_error().decode()  # noqa: E731
+    for k in (1, 2, 3):  # Y in Q, K, V
+        assert _forward(_desc(), Y=at(k)) == binding.MCA_ERR_INVALID_ARGUMENT and "operand" in said()
+    assert _forward(_desc(), lse=at(4).data) == binding.MCA_ERR_INVALID_ARGUMENT and "two results" in said()
+    for n, name in enumerate(("dQ", "dK", "dV")):
+        for k in range(1, 6):
+            assert _backward(_desc(), **{name: at(k)}) == binding.MCA_ERR_INVALID_ARGUMENT and "operand" in said(), name
+        other = at(6 + (n + 1) % 3)
+        assert _backward(_desc(), **{name: other}) == binding.MCA_ERR_INVALID_ARGUMENT and "two results" in said(), name
+    d = _desc(bias_table=FAKE, bias_buckets=32, bias_max_distance=128, bias_bidirectional=1)
+    assert _backward(d, lse=FAKE + (1 << 42), dbias=FAKE) == binding.MCA_ERR_INVALID_ARGUMENT and "operand" in said()
+
+
+def test_wide_integers_refused():
+    for args in ((8, 2**32 + 20), (2**32 + 8, 20), (8, 10**15)):
+        with pytest.raises(ValueError):
+            mca.relative_buckets(*args)
+    with pytest.raises(binding.MCAError):
+        mca.relative_buckets(8, 2**31 - 1)
 
 
 def test_other_arguments_refused():
