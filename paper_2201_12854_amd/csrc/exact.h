@@ -77,6 +77,7 @@ hipError_t exact_set_lds(size_t lds) {
 inline bool exact_worth(int64_t tiles, int64_t n, int unit) {
   return ((tiles + 3) / 4 - (tiles + 4 * n - 1) / (4 * n)) * unit >= 6;
 }
+bool exact_eight_waves(int64_t blocks, int64_t tiles);  // of the kernels of 32 rows, for a block's tiles
 int exact_splits(const ExactParams& p);
 int exact_kv_splits(const ExactParams& p);
 bool exact_backward_small(const ExactParams& p);  // in one launch, without a workspace

@@ -15,9 +15,9 @@ namespace mca {
 namespace {
 
 // ST: tiles in LDS per wave of the kernels of 32 rows, all but one of them on their way.
-template <typename T, int ST> constexpr int kDqLds = kExWaves * ST * 2 * tile_bytes<T>();
+template <typename T, int ST, int W> constexpr int kDqLds = W * ST * 2 * tile_bytes<T>();
 template <typename T> constexpr int kDkvStage = 2 * tile_bytes<T>() + 512;  // Q, dY, two planes of statistics
-template <typename T, int ST> constexpr int kDkvLds = kExWaves * ST * kDkvStage<T>;
+template <typename T, int ST, int W> constexpr int kDkvLds = W * ST * kDkvStage<T>;
 constexpr int kYS = kDHead + 4;  // row pitch of the sums that the waves of a block join in LDS
 
 // Four consecutive values of a row to `o`.
@@ -35,10 +35,11 @@ __device__ __forceinline__ void ex_put_sums(float* ys, const f32x16_t (&y)[2], i
           make_float4(y[cc][r], y[cc][r + 1], y[cc][r + 2], y[cc][r + 3]);
 }
 // Four columns of a row, summed over the waves in their order.
+template <int W>
 __device__ __forceinline__ float4 ex_join_sums(const float* ys, int row, int col, float scale) {
   float4 v = *reinterpret_cast<const float4*>(ys + row * kYS + col);
 #pragma unroll
-  for (int k = 1; k < kExWaves; ++k) {
+  for (int k = 1; k < W; ++k) {
     const float4 t = *reinterpret_cast<const float4*>(ys + (k * 32 + row) * kYS + col);
     v.x += t.x, v.y += t.y, v.z += t.z, v.w += t.w;
   }
@@ -206,12 +207,12 @@ bool few(const ExactParams& p) { return p.bf16 && std::min(p.nq, p.nk) <= 32; }
 // comes from large P, and is multiplied by them: the kernel of 64-row tiles leaves half tiles out of sum_j P k
 // whose P are all at most kSmallP (at 4 x 4096 tokens, 12 heads, all of them: dQ 317 us without this, 427
 // with every tile's product).
-template <typename T, bool BIAS, int ST, bool FEW>
+template <typename T, bool BIAS, int ST, int W, bool FEW>
 __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, int vt, int hx, int b, int Gp) {
   constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>();
   const int n = 2 * p.D + 129;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  float* tb = reinterpret_cast<float*>(smem + kDqLds<T, ST>);  // [Gp][n]
+  float* tb = reinterpret_cast<float*>(smem + kDqLds<T, ST, W>);  // [Gp][n]
   const int c = lane & 31, hf = lane >> 5;
   const ExRow0 br = ex_batch_row(p, b);
   const int hk = hx * Gp / p.G;
@@ -232,7 +233,7 @@ __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, in
                     lane);
   };
 #pragma unroll
-  for (int k = 0; k < ST - 1; ++k) load(wave + k * kExWaves, k);
+  for (int k = 0; k < ST - 1; ++k) load(wave + k * W, k);
 
   const int64_t hcol = head * kDHead;
   const char* qrow = static_cast<const char*>(p.Q.data) + (b * p.Q.batch + i * p.Q.row + hcol) * ES;
@@ -259,9 +260,9 @@ __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, in
   f32x16_t dq[2] = {ex_zero16(), ex_zero16()}, pk[2] = {ex_zero16(), ex_zero16()};
 
   int slot = 0;
-  for (int idx = wave; idx < tiles.n; idx += kExWaves) {
+  for (int idx = wave; idx < tiles.n; idx += W) {
     wait_lds();  // the tile read last is overwritten by the next loads
-    load(idx + (ST - 1) * kExWaves, slot == 0 ? ST - 1 : slot - 1);
+    load(idx + (ST - 1) * W, slot == 0 ? ST - 1 : slot - 1);
     wait_vmcnt<(ST - 1) * 2 * ExFmt<T>::NL>();
     asm volatile("" ::: "memory");
     char* kt = smem + (wave * ST + slot) * 2 * TB;
@@ -300,13 +301,13 @@ __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, in
   __syncthreads();
   float* ys = reinterpret_cast<float*>(smem);
   if constexpr (ES == 2) {
-    float* rests = ys + kExWaves * 32 * kYS;  // [wave][row]
+    float* rests = ys + W * 32 * kYS;  // [wave][row]
     rest += ex_other_half(rest);
     if (hf == 0) rests[wave * 32 + c] = rest;
     __syncthreads();
     rest = 0.f;
 #pragma unroll
-    for (int k = 0; k < kExWaves; ++k) rest += rests[k * 32 + c];
+    for (int k = 0; k < W; ++k) rest += rests[k * 32 + c];
     D += rest;
 #pragma unroll
     for (int cc = 0; cc < 2; ++cc)
@@ -318,20 +319,20 @@ __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, in
   if (wave == 0 && hf == 0 && i < p.nq) ex_put_stat<T>(p, ((int64_t)b * p.H + head) * p.nq + i, cr, D);
   __syncthreads();
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int row = (threadIdx.x >> 4) + half * 16, col = (threadIdx.x & 15) * 4;
+  for (int half = 0; half < 8 / W; ++half) {
+    const int row = (threadIdx.x >> 4) + half * 4 * W, col = (threadIdx.x & 15) * 4;
     const int vr = vt * 32 + row, ir = vr / Gp;
     if (ir < p.nq)
       ex_store4(static_cast<T*>(p.dQ.data) + b * p.dQ.batch + ir * p.dQ.row + (hx * Gp + vr % Gp) * kDHead + col,
-                ex_join_sums(ys, row, col, p.scale));
+                ex_join_sums<W>(ys, row, col, p.scale));
   }
 }
 
-template <typename T, bool BIAS, int ST, bool FEW = false>
-__global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
+template <typename T, bool BIAS, int ST, int W, bool FEW = false>
+__global__ __launch_bounds__(64 * W) void k_exact_dq(ExactParams p) {
   extern __shared__ __align__(16) char smem[];
   const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp, bid = blockIdx.x / nvt;
-  ex_dq_block<T, BIAS, ST, FEW>(p, smem, blockIdx.x % nvt, bid % Hx, bid / Hx, p.Gp);
+  ex_dq_block<T, BIAS, ST, W, FEW>(p, smem, blockIdx.x % nvt, bid % Hx, bid / Hx, p.Gp);
 }
 
 // ------------------------------------------------------------------ dK, dV
@@ -339,14 +340,14 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dq(ExactParams p) {
 // block's part of them (kv_splits). S = Q K^T and dP = dY V^T with the lane holding a key: P and dS
 // feed dV^T = dY^T P and dK^T = Q^T dS. A wave loads its tiles of Q, dY and row statistics straight
 // into LDS.
-template <typename T, bool BIAS, int ST, bool FEW>
+template <typename T, bool BIAS, int ST, int W, bool FEW>
 __device__ __forceinline__ void ex_dkv_block(const ExactParams& p, char* smem, int kt, int hk, int b, int split, int splits,
                                              int64_t part, int heads_at_once) {
   constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>(), SB = kDkvStage<T>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hf = lane >> 5, n = 2 * p.D + 129;
-  ExDiag diag{reinterpret_cast<float*>(smem + kDkvLds<T, ST>) + wave * n, 0.f, -1};
-  float* tb = reinterpret_cast<float*>(smem + kDkvLds<T, ST>) + kExWaves * n;  // [heads_at_once][n]
+  ExDiag diag{reinterpret_cast<float*>(smem + kDkvLds<T, ST, W>) + wave * n, 0.f, -1};
+  float* tb = reinterpret_cast<float*>(smem + kDkvLds<T, ST, W>) + W * n;  // [heads_at_once][n]
   const ExRow0 br = ex_batch_row(p, b);
   const int j = kt * 32 + c, jmax = min(kt * 32 + 31, br.klen - 1);
   const ExTiles tiles = ex_query_tiles(p, br, kt * 32, jmax);
@@ -388,11 +389,11 @@ __device__ __forceinline__ void ex_dkv_block(const ExactParams& p, char* smem, i
       ex_load_lds4(ex_rsrc(st + 4 * (int64_t)p.B * p.H * p.nq, 4, i0, limit, 4), lane * 4, to + 2 * TB + 256);
     };
 #pragma unroll
-    for (int k = 0; k < ST - 1; ++k) load(first + k * kExWaves, k);
+    for (int k = 0; k < ST - 1; ++k) load(first + k * W, k);
     int slot = 0;
-    for (int idx = first; idx < total; idx += kExWaves) {
+    for (int idx = first; idx < total; idx += W) {
       wait_lds();  // the tile read last is overwritten by the next loads
-      load(idx + (ST - 1) * kExWaves, slot == 0 ? ST - 1 : slot - 1);
+      load(idx + (ST - 1) * W, slot == 0 ? ST - 1 : slot - 1);
       wait_vmcnt<(ST - 1) * (2 * ExFmt<T>::NL + 2)>();
       asm volatile("" ::: "memory");
       const char* qt = smem + (wave * ST + slot) * SB;
@@ -474,15 +475,15 @@ __device__ __forceinline__ void ex_dkv_block(const ExactParams& p, char* smem, i
     ex_put_sums(ys, which ? dv : dk, wave * 32 + c, hf);
     __syncthreads();
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int row = (threadIdx.x >> 4) + half * 16, col = (threadIdx.x & 15) * 4, jr = kt * 32 + row;
+    for (int half = 0; half < 8 / W; ++half) {
+      const int row = (threadIdx.x >> 4) + half * 4 * W, col = (threadIdx.x & 15) * 4, jr = kt * 32 + row;
       if (jr >= p.nk) continue;
       if (splits > 1) {
         const int64_t at = (((int64_t)(split * p.B + b) * p.nk + jr) * p.Hk + hk) * kDHead + col;
-        ex_store4((which ? p.part_dv : p.part_dk) + at, ex_join_sums(ys, row, col, 1.f));
+        ex_store4((which ? p.part_dv : p.part_dk) + at, ex_join_sums<W>(ys, row, col, 1.f));
       } else {
         const ExactOut& t = which ? p.dV : p.dK;
-        const float4 v = ex_join_sums(ys, row, col, which ? 1.f : p.scale);
+        const float4 v = ex_join_sums<W>(ys, row, col, which ? 1.f : p.scale);
         ex_store4(static_cast<T*>(t.data) + b * t.batch + jr * t.row + hk * kDHead + col,
                   jr < br.klen ? v : make_float4(0.f, 0.f, 0.f, 0.f));
       }
@@ -490,8 +491,8 @@ __device__ __forceinline__ void ex_dkv_block(const ExactParams& p, char* smem, i
   }
 }
 
-template <typename T, bool BIAS, int ST, bool FEW = false>
-__global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int heads_at_once) {
+template <typename T, bool BIAS, int ST, int W, bool FEW = false>
+__global__ __launch_bounds__(64 * W) void k_exact_dkv(ExactParams p, int heads_at_once) {
   extern __shared__ __align__(16) char smem[];
   const int nkt = (p.nk + 31) / 32;
   int bid = blockIdx.x;
@@ -499,8 +500,8 @@ __global__ __launch_bounds__(kExThreads) void k_exact_dkv(ExactParams p, int hea
   bid /= nkt;
   const int hk = bid % p.Hk;
   bid /= p.Hk;
-  const int64_t part = ((int64_t)bid * nkt + kt) * kExWaves;  // bid: split * B + batch row
-  ex_dkv_block<T, BIAS, ST, FEW>(p, smem, kt, hk, bid % p.B, bid / p.B, p.kv_splits, part, heads_at_once);
+  const int64_t part = ((int64_t)bid * nkt + kt) * W;  // bid: split * B + batch row
+  ex_dkv_block<T, BIAS, ST, W, FEW>(p, smem, kt, hk, bid % p.B, bid / p.B, p.kv_splits, part, heads_at_once);
 }
 
 // ------------------------------------------------------------------ tiles of 64 rows, bf16
@@ -543,7 +544,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   if constexpr (WIN) {  // the first blocks: the rows around a global query
     if (bid < p.H * p.B) {
       const int first = ex_global_rows(p, ex_batch_row(p, bid / p.H));
-      if (first >= 0) ex_dq_block<uint16_t, BIAS, 2, false>(p, smem, first / 32, bid % p.H, bid / p.H, 1);
+      if (first >= 0) ex_dq_block<uint16_t, BIAS, 2, 4, false>(p, smem, first / 32, bid % p.H, bid / p.H, 1);
       return;
     }
     bid -= p.H * p.B;
@@ -735,7 +736,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   if constexpr (WIN) {  // the first blocks: the keys around the global one (kv_splits is 1)
     if (bid < p.Hk * p.B) {
       const int64_t part = ((int64_t)p.B * nkt + bid / p.Hk) * kExWaves;
-      ex_dkv_block<uint16_t, BIAS, 2, false>(p, smem, 0, bid % p.Hk, bid / p.Hk, 0, 1, part, heads_at_once);
+      ex_dkv_block<uint16_t, BIAS, 2, 4, false>(p, smem, 0, bid % p.Hk, bid / p.Hk, 0, 1, part, heads_at_once);
       return;
     }
     bid -= p.Hk * p.B;
@@ -1174,21 +1175,37 @@ bool dkv_in_tiles(const ExactParams& p) {
   return in_tiles(p, (int64_t)((p.nk + 31) / 32) * p.Hk * p.B, p.G * p.nq) || (p.bf16 && (int64_t)p.G * ((p.nq + 31) / 32) > 64);
 }
 
+int dkv_waves(const ExactParams& p) {  // of k_exact_dkv
+  const int64_t tiles = (int64_t)p.G * ((p.nq + 31) / 32) / p.kv_splits;
+  return p.bf16 && !few(p) && exact_eight_waves((int64_t)((p.nk + 31) / 32) * p.Hk * p.B * p.kv_splits, tiles) ? 8 : 4;
+}
+
 // The largest table (and a wave's sums along diagonals, as long) fits beside the tiles.
 constexpr size_t kMaxTable = (2 * kMaxBiasDistance + 129) * 4;
-static_assert(kDkvLds<float, 2> + (kExWaves + 1) * kMaxTable <= kMaxLds && kDkvLds<uint16_t, 2> + (kExWaves + 1) * kMaxTable <= kMaxLds &&
-              kDkvTilesLds + (kExWaves + 1) * kMaxTable <= kMaxLds / 2, "LDS of a block");
+static_assert(kDkvLds<float, 2, 4> + 5 * kMaxTable <= kMaxLds && kDkvLds<uint16_t, 2, 4> + 5 * kMaxTable <= kMaxLds &&
+              kDkvLds<uint16_t, 2, 8> + 9 * kMaxTable <= kMaxLds &&
+              kDkvTilesLds + 5 * kMaxTable <= kMaxLds / 2, "LDS of a block");
+
+template <typename T, bool BIAS, int ST, int W, bool FEW = false>
+hipError_t launch_dq_of(const ExactParams& p, hipStream_t s) {
+  const size_t lds = kDqLds<T, ST, W> + (BIAS ? (size_t)p.Gp * exact_bias_entries(p.D) * 4 : 0);
+  const hipError_t e = exact_set_lds<k_exact_dq<T, BIAS, ST, W, FEW>>(lds);
+  if (e != hipSuccess) return e;
+  const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
+  hipLaunchKernelGGL((k_exact_dq<T, BIAS, ST, W, FEW>), dim3((unsigned)blocks), dim3(64 * W), lds, s, p);
+  return hipGetLastError();
+}
 
 template <typename T, bool BIAS>
 hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
-  const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
-  hipError_t e;
   if constexpr (ExFmt<T>::ES == 2) {
     if (dq_in_tiles(p)) {
+      const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
       const int64_t blocks = (int64_t)((p.nq + 127) / 128) * p.H * p.B;
       if (p.window && !p.causal) {
-        const size_t lds = kDqLds<T, 2> + table;
-        if ((e = exact_set_lds<k_exact_dq_tiles<BIAS, true>>(lds)) != hipSuccess) return e;
+        const size_t lds = kDqLds<T, 2, 4> + table;
+        const hipError_t e =  exact_set_lds<k_exact_dq_tiles<BIAS, true>>(lds);
+        if (e != hipSuccess) return e;
         hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, true>), dim3((unsigned)(blocks + p.H * p.B)), dim3(kExThreads), lds, s, p);
       } else {
         hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, false>), dim3((unsigned)blocks), dim3(kExThreads), 6 * kTile64 + table, s, p);
@@ -1196,26 +1213,21 @@ hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
       return hipGetLastError();
     }
   }
-  const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
-  const size_t one = kDqLds<T, 1> + table * p.Gp, two = kDqLds<T, 2> + table * p.Gp;
-  auto launch = [&](auto kernel, hipError_t set, size_t lds) {
-    if (set != hipSuccess) return set;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
-    return hipGetLastError();
-  };
+  const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B, tiles = (p.nk + 31) / 32;
   if constexpr (ExFmt<T>::ES == 4) {  // as the forward pass
-    if (blocks > device_cus()) return launch(k_exact_dq<T, BIAS, 1>, exact_set_lds<k_exact_dq<T, BIAS, 1>>(one), one);
+    if (blocks > device_cus()) return launch_dq_of<T, BIAS, 1, 4>(p, s);
   } else {
-    if (few(p)) return launch(k_exact_dq<T, BIAS, 2, true>, exact_set_lds<k_exact_dq<T, BIAS, 2, true>>(two), two);
+    if (few(p)) return launch_dq_of<T, BIAS, 2, 4, true>(p, s);
+    if (exact_eight_waves(blocks, tiles)) return launch_dq_of<T, BIAS, 2, 8>(p, s);
   }
-  return launch(k_exact_dq<T, BIAS, 2>, exact_set_lds<k_exact_dq<T, BIAS, 2>>(two), two);
+  return launch_dq_of<T, BIAS, 2, 4>(p, s);
 }
 
 // A block's tiles and its waves' sums along diagonals in LDS, then the bias tables of as many heads as fit.
-template <auto K, bool BIAS>
+template <auto K, bool BIAS, int W = kExWaves>
 hipError_t launch_dkv_kernel(const ExactParams& p, int keys, size_t base, hipStream_t s, int more = 0) {
   const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
-  base += kExWaves * table;
+  base += W * table;
   int heads = p.G;
   if constexpr (BIAS) {
     const size_t room = base + table <= kMaxLds / 2 ? kMaxLds / 2 : kMaxLds;  // two blocks to a CU, or one
@@ -1225,23 +1237,28 @@ hipError_t launch_dkv_kernel(const ExactParams& p, int keys, size_t base, hipStr
   const hipError_t e = exact_set_lds<K>(lds);
   if (e != hipSuccess) return e;
   const int64_t blocks = (int64_t)((p.nk + keys - 1) / keys) * p.Hk * p.B * p.kv_splits + more;
-  hipLaunchKernelGGL(K, dim3((unsigned)blocks), dim3(kExThreads), lds, s, p, heads);
+  hipLaunchKernelGGL(K, dim3((unsigned)blocks), dim3(64 * W), lds, s, p, heads);
   return hipGetLastError();
+}
+
+template <typename T, bool BIAS, int ST, int W, bool FEW = false>
+hipError_t launch_dkv_of(const ExactParams& p, hipStream_t s) {
+  return launch_dkv_kernel<k_exact_dkv<T, BIAS, ST, W, FEW>, BIAS, W>(p, 32, kDkvLds<T, ST, W>, s);
 }
 
 template <typename T, bool BIAS>
 hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
   hipError_t e = hipErrorInvalidValue;
   if (!dkv_in_tiles(p)) {
-    e = hipErrorNotReady;
-    if constexpr (ExFmt<T>::ES == 4)  // (as the forward pass)
-      if ((int64_t)((p.nk + 31) / 32) * p.Hk * p.B * p.kv_splits > device_cus())
-        e = launch_dkv_kernel<k_exact_dkv<T, BIAS, 1>, BIAS>(p, 32, kDkvLds<T, 1>, s);
-    if constexpr (ExFmt<T>::ES == 2)
-      if (few(p)) e = launch_dkv_kernel<k_exact_dkv<T, BIAS, 2, true>, BIAS>(p, 32, kDkvLds<T, 2>, s);
-    if (e == hipErrorNotReady) e = launch_dkv_kernel<k_exact_dkv<T, BIAS, 2>, BIAS>(p, 32, kDkvLds<T, 2>, s);
+    const int64_t blocks = (int64_t)((p.nk + 31) / 32) * p.Hk * p.B * p.kv_splits;
+    if constexpr (ExFmt<T>::ES == 4) {  // as the forward pass
+      e = blocks > device_cus() ? launch_dkv_of<T, BIAS, 1, 4>(p, s) : launch_dkv_of<T, BIAS, 2, 4>(p, s);
+    } else {
+      e = few(p) ? launch_dkv_of<T, BIAS, 2, 4, true>(p, s)
+                 : dkv_waves(p) == 8 ? launch_dkv_of<T, BIAS, 2, 8>(p, s) : launch_dkv_of<T, BIAS, 2, 4>(p, s);
+    }
   } else if constexpr (ExFmt<T>::ES == 2) {
-    if (p.window) e = launch_dkv_kernel<k_exact_dkv_tiles<BIAS, true>, BIAS>(p, 128, kDkvLds<T, 2>, s, p.Hk * p.B);
+    if (p.window) e = launch_dkv_kernel<k_exact_dkv_tiles<BIAS, true>, BIAS>(p, 128, kDkvLds<T, 2, 4>, s, p.Hk * p.B);
     else e = launch_dkv_kernel<k_exact_dkv_tiles<BIAS, false>, BIAS>(p, 128, kDkvTilesLds, s);
   }
   if (e != hipSuccess) return e;
@@ -1287,7 +1304,7 @@ int exact_kv_splits(const ExactParams& p) {
 }
 
 int64_t exact_bias_parts(const ExactParams& p) {  // a part per wave of k_exact_dkv
-  if (!dkv_in_tiles(p)) return (int64_t)p.kv_splits * p.B * ((p.nk + 31) / 32) * kExWaves;
+  if (!dkv_in_tiles(p)) return (int64_t)p.kv_splits * p.B * ((p.nk + 31) / 32) * dkv_waves(p);
   return (int64_t)p.B * (p.kv_splits * ((p.nk + 127) / 128) + (p.window ? 1 : 0)) * kExWaves;
 }
 

@@ -46,17 +46,17 @@ __device__ __forceinline__ void ex_softmax_step(ExState& s, f32x16_t& x) {
 
 // ------------------------------------------------------------------ 32 rows per block
 // Blocks of 32 (query, head) rows: a key head's Gp query heads side by side, so that the keys are read
-// once for them. The key tiles are dealt out to the block's four waves and to `splits` blocks; a
+// once for them. The key tiles are dealt out to the block's waves and to `splits` blocks; a
 // wave loads its own tiles straight into LDS ahead of their use and waits for nobody until the
 // end, where the waves' states (and the blocks', in k_exact_join) are joined in a fixed order.
-template <typename T, int ST> constexpr int kRowLds = kExWaves * ST * 2 * tile_bytes<T>();
+template <typename T, int ST, int W> constexpr int kRowLds = W * ST * 2 * tile_bytes<T>();
 
-// ST: tiles in LDS per wave, all but one of them on their way.
-template <typename T, bool BIAS, int ST, bool FEW>
+// ST: tiles in LDS per wave, all but one of them on their way. W: waves of the block.
+template <typename T, bool BIAS, int ST, int W, bool FEW>
 __device__ __forceinline__ void ex_rows_block(const ExactParams& p, char* smem, int vt, int hx, int b, int split, int splits,
                                               int Gp) {
   constexpr int ES = ExFmt<T>::ES, TB = tile_bytes<T>();
-  float* tb = reinterpret_cast<float*>(smem + kRowLds<T, ST>);
+  float* tb = reinterpret_cast<float*>(smem + kRowLds<T, ST, W>);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hf = lane >> 5;
   const int nvt = (int)((p.nq * Gp + 31) / 32), Hx = p.H / Gp;
@@ -72,14 +72,14 @@ __device__ __forceinline__ void ex_rows_block(const ExactParams& p, char* smem, 
   const char* Kb = static_cast<const char*>(p.K.data) + (b * p.K.batch + hk * kDHead) * ES;
   const char* Vb = static_cast<const char*>(p.V.data) + (b * p.V.batch + hk * kDHead) * ES;
   const uint32_t lds = lds_addr(smem) + (uint32_t)wave * ST * 2 * TB;
-  const int step = kExWaves * splits;
+  const int step = W * splits;
   auto load = [&](int idx, int slot) __attribute__((always_inline)) {  // past the last tile: zeros
     const int k0 = ex_tile_at(tiles, idx) * 32, limit = idx < tiles.n ? br.klen : 0;
     ex_load_tile<T>(ex_rsrc(Kb, p.K.row * ES, k0, limit, ExFmt<T>::RB), (int)p.K.row * ES, lds + slot * 2 * TB, lane);
     ex_load_tile<T>(ex_rsrc(Vb, p.V.row * ES, k0, limit, ExFmt<T>::RB), (int)p.V.row * ES, lds + slot * 2 * TB + TB,
                     lane);
   };
-  const int idx0 = split * kExWaves + wave;
+  const int idx0 = split * W + wave;
 #pragma unroll
   for (int k = 0; k < ST - 1; ++k) load(idx0 + k * step, k);
 
@@ -135,7 +135,7 @@ __device__ __forceinline__ void ex_rows_block(const ExactParams& p, char* smem, 
   // states of the waves in LDS: [wave][row][68] sums, [wave][row] (m, l)
   constexpr int YS = kDHead + 4;
   float* ys = reinterpret_cast<float*>(smem);
-  float2* ml = reinterpret_cast<float2*>(smem + kExWaves * 32 * YS * 4);
+  float2* ml = reinterpret_cast<float2*>(smem + W * 32 * YS * 4);
 #pragma unroll
   for (int cc = 0; cc < 2; ++cc)
 #pragma unroll
@@ -144,17 +144,17 @@ __device__ __forceinline__ void ex_rows_block(const ExactParams& p, char* smem, 
           make_float4(s.y[cc][r], s.y[cc][r + 1], s.y[cc][r + 2], s.y[cc][r + 3]);
   if (hf == 0) ml[wave * 32 + c] = make_float2(s.m, s.l);
   __syncthreads();
-  // thread: 4 columns of two rows
+  // thread: 4 columns of a row, or of two
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int row = (threadIdx.x >> 4) + half * 16, col = (threadIdx.x & 15) * 4;
+  for (int half = 0; half < 8 / W; ++half) {
+    const int row = (threadIdx.x >> 4) + half * 4 * W, col = (threadIdx.x & 15) * 4;
     float M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int k = 0; k < kExWaves; ++k) M = fmaxf(M, ml[k * 32 + row].x);
+    for (int k = 0; k < W; ++k) M = fmaxf(M, ml[k * 32 + row].x);
     const float ref = M == -INFINITY ? 0.f : M;
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < kExWaves; ++k) {
+    for (int k = 0; k < W; ++k) {
       const float w = ex_exp2(ml[k * 32 + row].x - ref);
       L += ml[k * 32 + row].y * w;
       const float4 t = *reinterpret_cast<const float4*>(ys + (k * 32 + row) * YS + col);
@@ -179,8 +179,8 @@ __device__ __forceinline__ void ex_rows_block(const ExactParams& p, char* smem, 
   }
 }
 
-template <typename T, bool BIAS, int ST, bool FEW>
-__global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
+template <typename T, bool BIAS, int ST, int W, bool FEW>
+__global__ __launch_bounds__(64 * W) void k_exact_rows(ExactParams p) {
   extern __shared__ __align__(16) char smem[];
   const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp;
   int bid = blockIdx.x;
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_rows(ExactParams p) {
   bid /= nvt;
   const int hx = bid % Hx;
   bid /= Hx;
-  ex_rows_block<T, BIAS, ST, FEW>(p, smem, vt, hx, bid % p.B, bid / p.B, p.splits, p.Gp);
+  ex_rows_block<T, BIAS, ST, W, FEW>(p, smem, vt, hx, bid % p.B, bid / p.B, p.splits, p.Gp);
 }
 
 // Joins the parts (at most 64) of a (query, head) row: a wave per row, a lane per part for the weights and per
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
   if constexpr (WIN) {  // the first blocks: the rows around a global query
     if (bid < p.H * p.B) {
       const int first = ex_global_rows(p, ex_batch_row(p, bid / p.H));
-      if (first >= 0) ex_rows_block<uint16_t, BIAS, 2, false>(p, smem, first / 32, bid % p.H, bid / p.H, 0, 1, 1);
+      if (first >= 0) ex_rows_block<uint16_t, BIAS, 2, 4, false>(p, smem, first / 32, bid % p.H, bid / p.H, 0, 1, 1);
       return;
     }
     bid -= p.H * p.B;
@@ -498,7 +498,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
 template <bool BIAS, int MT, bool WIN>
 hipError_t launch_tiles(const ExactParams& p, hipStream_t s) {
   const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
-  const size_t lds = table + (WIN ? (size_t)kRowLds<uint16_t, 2> : 6 * kTile64);
+  const size_t lds = table + (WIN ? (size_t)kRowLds<uint16_t, 2, 4> : 6 * kTile64);
   const int64_t blocks = ((int64_t)((p.nq + 128 * MT - 1) / (128 * MT)) + WIN) * p.H * p.B;
   if constexpr (WIN) {
     const hipError_t e = exact_set_lds<k_exact_tiles<BIAS, MT, WIN>, 512>(lds);
@@ -509,13 +509,13 @@ hipError_t launch_tiles(const ExactParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, bool BIAS, int ST, bool FEW = false>
+template <typename T, bool BIAS, int ST, int W, bool FEW = false>
 hipError_t launch_rows_of(const ExactParams& p, hipStream_t s) {
-  const size_t lds = kRowLds<T, ST> + (BIAS ? (size_t)p.Gp * exact_bias_entries(p.D) * 4 : 0);
-  hipError_t e = exact_set_lds<k_exact_rows<T, BIAS, ST, FEW>>(lds);
+  const size_t lds = kRowLds<T, ST, W> + (BIAS ? (size_t)p.Gp * exact_bias_entries(p.D) * 4 : 0);
+  hipError_t e = exact_set_lds<k_exact_rows<T, BIAS, ST, W, FEW>>(lds);
   if (e != hipSuccess) return e;
   const int64_t rows = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
-  hipLaunchKernelGGL((k_exact_rows<T, BIAS, ST, FEW>), dim3((unsigned)(rows * p.splits)), dim3(kExThreads), lds, s, p);
+  hipLaunchKernelGGL((k_exact_rows<T, BIAS, ST, W, FEW>), dim3((unsigned)(rows * p.splits)), dim3(64 * W), lds, s, p);
   if ((e = hipGetLastError()) != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL((k_exact_join<T>), dim3((unsigned)(((int64_t)p.B * p.H * p.nq + kExWaves - 1) / kExWaves)), dim3(kExThreads), 0, s, p);
   return hipGetLastError();
@@ -530,11 +530,14 @@ constexpr int kFewKeys = 128;
 // (forward, 12 heads: 2 x 333 tokens, one block to a CU, 14.6 against 15.5 us; 32 x 128, six, 48 against 36).
 template <typename T, bool BIAS>
 hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
-  if constexpr (ExFmt<T>::ES == 4)
-    if (exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B * p.splits > device_cus()) return launch_rows_of<T, BIAS, 1>(p, s);
-  if constexpr (ExFmt<T>::ES == 2)
-    if (p.nk <= kFewKeys) return launch_rows_of<T, BIAS, 2, true>(p, s);
-  return launch_rows_of<T, BIAS, 2>(p, s);
+  const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B * p.splits;
+  if constexpr (ExFmt<T>::ES == 4) {
+    if (blocks > device_cus()) return launch_rows_of<T, BIAS, 1, 4>(p, s);
+  } else {
+    if (p.nk <= kFewKeys) return launch_rows_of<T, BIAS, 2, 4, true>(p, s);
+    if (exact_eight_waves(blocks, ((p.nk + 31) / 32) / p.splits)) return launch_rows_of<T, BIAS, 2, 8>(p, s);
+  }
+  return launch_rows_of<T, BIAS, 2, 4>(p, s);
 }
 
 }  // namespace
@@ -542,7 +545,7 @@ hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
 // Heads side by side in the kernels of 32 rows: a key head's whole group, unless its bias tables do not
 // fit beside the tiles.
 int exact_group(const ExactParams& p) {
-  return !p.table || (int64_t)p.G * exact_bias_entries(p.D) * 4 <= (int64_t)kMaxLds - kRowLds<float, 2> ? p.G : 1;
+  return !p.table || (int64_t)p.G * exact_bias_entries(p.D) * 4 <= (int64_t)kMaxLds - kRowLds<float, 2, 4> ? p.G : 1;
 }
 
 // bf16 in blocks of 128 queries or more: where the blocks of 32 rows are more than the CUs (forward, 12
@@ -578,6 +581,13 @@ int exact_splits(const ExactParams& p) {
   const int64_t n = std::min<int64_t>(std::max<int64_t>(std::max(fill, even), 1), 64);
   return exact_worth(tiles, n, p.bf16 ? 1 : 4) ? (int)n : 1;
 }
+
+// Eight waves to a block instead of four, bf16: where every block has a CU of its own and more than two tiles to
+// a wave (a token, 12 heads: 1024 keys 9.7 us with four waves, 8.3 with eight, 701 keys 8.5 and 7.6, 300 keys,
+// 10 tiles, 6.7 and 6.6; 2 x 1024 tokens, 4 heads, forward 10.5 and 9.2, backward 27.8 and 24.7; backward
+// 2 x 256, 8 tiles, 15.0 and 16.6). Not float32, which its matrix instructions bound: 1 x 512 tokens, forward
+// and backward, 74 and 72; 4 x 201, 8 heads on 2, with a bias, 59 and 61.
+bool exact_eight_waves(int64_t blocks, int64_t tiles) { return tiles > 8 && blocks <= device_cus(); }
 
 hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s) {
   if (forward_in_tiles(p)) {

@@ -66,6 +66,11 @@ SHAPES = [  # B, nq, nk, heads, kv_heads, options
     (2, 150, 150, 2, 2, dict(window=30, causal=True)),
     (2, 40, 200, 2, 2, dict(window=30, causal=True, q_pos=[-10, 100])),
     (1, 513, 511, 2, 1, {}),
+    # more than eight tiles to a block and a CU to each: eight waves
+    (1, 1, 297, 4, 4, {}),
+    (2, 330, 330, 4, 4, dict(kv_lens=[330, 290], q_lens=[330, 289])),
+    (1, 300, 289, 6, 2, dict(causal=True)),
+    (1, 500, 500, 3, 3, dict(window=40)),
     # up to 128 queries and keys: one launch for the gradients in bfloat16
     (3, 128, 100, 4, 4, dict(window=16, q_lens=[128, 33, 1], kv_lens=[100, 64, 2])),
     (2, 100, 128, 3, 3, dict(window=30, causal=True, q_pos=[28, -40])),
