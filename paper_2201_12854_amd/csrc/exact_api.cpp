@@ -108,9 +108,10 @@ mca_status check_exact(const mca_exact_desc* d) {
     if (st != MCA_OK) return st;
   }
   if (d->d_head != 64) return fail(MCA_ERR_UNSUPPORTED, "d_head must be 64 (got %lld)", (long long)d->d_head);
-  // every launch of either pass, with the fewest heads side by side
+  // every launch of either pass, with the fewest heads side by side (float32: the rows' blocks, an eighth of all at
+  // most, and the keys' in one)
   const int64_t q = mca::exact_row_tiles(d->q_len, 1), k = (d->kv_len + 31) / 32;
-  if ((q * 8 > kMaxBlocks / d->heads / d->batch) || (k + 1 > (kMaxBlocks - mca::kMaxBuckets * 1024) / d->kv_heads / d->batch))
+  if ((q * 8 > kMaxBlocks / d->heads / d->batch) || (k + 1 > (kMaxBlocks / 8 * 7 - mca::kMaxBuckets * 1024) / d->kv_heads / d->batch))
     return fail(MCA_ERR_INVALID_ARGUMENT, "batch * heads * length too large for one launch");
   return MCA_OK;
 }

@@ -1,11 +1,13 @@
 // Exact attention, backward: the probabilities are taken again from the row log-sum-exp,
 //   P = exp2(s2 q.k + bias - c),  c = log2(e) lse,   dP = dY.v,   D = dY.y,   dS = P (dP - D),
 //   dq = scale sum_j dS k,   dk = scale sum_i dS q,   dv = sum_i P dy,   dT[c] = sum of dS in bucket c.
-// Two kernels, each summing over its own loop, so that every sum has a fixed order and no result
-// depends on the order of atomics: k_exact_dq (per query rows; also D) and k_exact_dkv (per keys, over
-// the query heads that share them; also the bias gradient). That takes S and dP twice: seven
-// products for the five that the formulas need. k_exact_join_grads adds up what the blocks of
-// k_exact_dkv leave in parts.
+// Two parts, each summing over its own loop, so that every sum has a fixed order and no result depends on the
+// order of atomics: dQ (per query rows) and dK, dV (per keys, over the query heads that share them; also the bias
+// gradient). That takes S and dP twice: seven products for the five that the formulas need. bf16: a launch
+// each, as the second needs a D that only the first has (below); up to 128 rows one launch of blocks that
+// have both. float32: k_exact_stats, then one launch of both parts' blocks, which fill the card together
+// (backward pass, 12 heads, a launch each against this: 2 x 333 tokens 64.3 and 50.4 us, 1 x 128 22.1 and
+// 13.9, 8 x 512 225 and 222). k_exact_join_grads adds up what blocks leave in parts.
 #include <algorithm>
 
 #include "exact_device.h"
@@ -14,7 +16,8 @@
 namespace mca {
 namespace {
 
-// ST: tiles in LDS per wave of the kernels of 32 rows, all but one of them on their way.
+// ST: tiles in LDS per wave of the blocks of 32 rows, all but one of them on their way: two in bf16, one in
+// float32, where two such blocks on a CU cover each other's loads. W: waves of the block.
 template <typename T, int ST, int W> constexpr int kDqLds = W * ST * 2 * tile_bytes<T>();
 template <typename T> constexpr int kDkvStage = 2 * tile_bytes<T>() + 512;  // Q, dY, two planes of statistics
 template <typename T, int ST, int W> constexpr int kDkvLds = W * ST * kDkvStage<T>;
@@ -46,12 +49,33 @@ __device__ __forceinline__ float4 ex_join_sums(const float* ys, int row, int col
   return make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
 }
 
-// What k_exact_dkv starts from.
-template <typename T>
+// What k_exact_dkv starts from, bf16.
 __device__ __forceinline__ void ex_put_stat(const ExactParams& p, int64_t row, float c, float D) {
-  const int64_t plane = (int64_t)p.B * p.H * p.nq;
-  p.rowstat[row] = ExFmt<T>::ES == 2 ? -c * (1.f / p.s2) : c;
-  p.rowstat[plane + row] = ExFmt<T>::ES == 2 ? -D : D;
+  p.rowstat[row] = -c * (1.f / p.s2);
+  p.rowstat[(int64_t)p.B * p.H * p.nq + row] = -D;
+}
+// float32: c and D, 16 lanes a row.
+__global__ __launch_bounds__(kExThreads) void k_exact_stats(ExactParams p) {
+  const int64_t rows = (int64_t)p.B * p.nq * p.H, e = (int64_t)blockIdx.x * (kExThreads / 16) + (threadIdx.x >> 4);
+  if (e >= rows) return;  // (rows of 16 lanes leave together)
+  const int h = (int)(e % p.H), i = (int)(e / p.H % p.nq), b = (int)(e / p.H / p.nq);
+  const int64_t row = ((int64_t)b * p.H + h) * p.nq + i, col = h * kDHead + 4 * (threadIdx.x & 15);
+  float D = 0.f, c = INFINITY;  // as in ex_dq_block
+  if (i < ex_batch_row(p, b).qlen) {
+    const float4 y = *reinterpret_cast<const float4*>(static_cast<const float*>(p.Y.data) + b * p.Y.batch + i * p.Y.row + col);
+    const float4 g = *reinterpret_cast<const float4*>(static_cast<const float*>(p.dY.data) + b * p.dY.batch + i * p.dY.row + col);
+    D = fmaf(y.w, g.w, fmaf(y.z, g.z, fmaf(y.y, g.y, y.x * g.x)));
+    const float lse = p.lse[row];
+    c = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  }
+  D += dpp_f32<0xB1>(D);
+  D += dpp_f32<0x4E>(D);
+  D += dpp_f32<0x141>(D);
+  D += dpp_f32<0x140>(D);
+  if ((threadIdx.x & 15) == 0) {
+    p.rowstat[row] = c;
+    p.rowstat[(int64_t)p.B * p.H * p.nq + row] = D;
+  }
 }
 
 // ------------------------------------------------------------------ sums along diagonals
@@ -237,17 +261,23 @@ __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, in
 
   const int64_t hcol = head * kDHead;
   const char* qrow = static_cast<const char*>(p.Q.data) + (b * p.Q.batch + i * p.Q.row + hcol) * ES;
-  const char* yrow = static_cast<const char*>(p.Y.data) + (b * p.Y.batch + i * p.Y.row + hcol) * ES;
   const char* dyrow = static_cast<const char*>(p.dY.data) + (b * p.dY.batch + i * p.dY.row + hcol) * ES;
   const ExRow<T> q = live ? ex_global_row<T>(qrow, hf) : ex_zero_row<T>();
   const ExRow<T> dy = live ? ex_global_row<T>(dyrow, hf) : ex_zero_row<T>();
   float D = 0.f, cr = INFINITY;  // a row without keys, or behind the last query: every P is 0
   if (live) {
-    D = ex_row_dot<T>(dy, ex_global_row<T>(yrow, hf), D);
-    const float lse = p.lse[((int64_t)b * p.H + head) * p.nq + i];
-    cr = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    const int64_t row = ((int64_t)b * p.H + head) * p.nq + i;
+    if constexpr (ES == 2) {
+      const char* yrow = static_cast<const char*>(p.Y.data) + (b * p.Y.batch + i * p.Y.row + hcol) * ES;
+      D = ex_row_dot<T>(dy, ex_global_row<T>(yrow, hf), D);
+      const float lse = p.lse[row];
+      cr = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    } else {  // k_exact_stats has been here
+      cr = p.rowstat[row];
+      D = p.rowstat[(int64_t)p.B * p.H * p.nq + row];
+    }
   }
-  D += ex_other_half(D);
+  if constexpr (ES == 2) D += ex_other_half(D);
   const int pos = br.pos + i;
   const ExSpan keys = ex_keys_of(p, pos, br.klen);
   const float* tl = nullptr;
@@ -316,7 +346,8 @@ __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, in
   }
   if (!ex_has(ex_many_keys(p, br.klen), pos)) dq[0] = dq[1] = ex_zero16();
   ex_put_sums(ys, dq, wave * 32 + c, hf);
-  if (wave == 0 && hf == 0 && i < p.nq) ex_put_stat<T>(p, ((int64_t)b * p.H + head) * p.nq + i, cr, D);
+  if constexpr (ES == 2)
+    if (wave == 0 && hf == 0 && i < p.nq) ex_put_stat(p, ((int64_t)b * p.H + head) * p.nq + i, cr, D);
   __syncthreads();
 #pragma unroll
   for (int half = 0; half < 8 / W; ++half) {
@@ -328,11 +359,11 @@ __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, in
   }
 }
 
-template <typename T, bool BIAS, int ST, int W, bool FEW = false>
-__global__ __launch_bounds__(64 * W) void k_exact_dq(ExactParams p) {
+template <bool BIAS, int W, bool FEW>
+__global__ __launch_bounds__(64 * W) void k_exact_dq(ExactParams p) {  // bf16
   extern __shared__ __align__(16) char smem[];
   const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp, bid = blockIdx.x / nvt;
-  ex_dq_block<T, BIAS, ST, W, FEW>(p, smem, blockIdx.x % nvt, bid % Hx, bid / Hx, p.Gp);
+  ex_dq_block<uint16_t, BIAS, 2, W, FEW>(p, smem, blockIdx.x % nvt, bid % Hx, bid / Hx, p.Gp);
 }
 
 // ------------------------------------------------------------------ dK, dV
@@ -491,8 +522,8 @@ __device__ __forceinline__ void ex_dkv_block(const ExactParams& p, char* smem, i
   }
 }
 
-template <typename T, bool BIAS, int ST, int W, bool FEW = false>
-__global__ __launch_bounds__(64 * W) void k_exact_dkv(ExactParams p, int heads_at_once) {
+template <bool BIAS, int W, bool FEW>
+__global__ __launch_bounds__(64 * W) void k_exact_dkv(ExactParams p, int heads_at_once) {  // bf16
   extern __shared__ __align__(16) char smem[];
   const int nkt = (p.nk + 31) / 32;
   int bid = blockIdx.x;
@@ -501,7 +532,27 @@ __global__ __launch_bounds__(64 * W) void k_exact_dkv(ExactParams p, int heads_a
   const int hk = bid % p.Hk;
   bid /= p.Hk;
   const int64_t part = ((int64_t)bid * nkt + kt) * W;  // bid: split * B + batch row
-  ex_dkv_block<T, BIAS, ST, W, FEW>(p, smem, kt, hk, bid % p.B, bid / p.B, p.kv_splits, part, heads_at_once);
+  ex_dkv_block<uint16_t, BIAS, 2, W, FEW>(p, smem, kt, hk, bid % p.B, bid / p.B, p.kv_splits, part, heads_at_once);
+}
+
+// float32: both in one launch, behind k_exact_stats, the keys' blocks first.
+template <bool BIAS>
+__global__ __launch_bounds__(kExThreads) void k_exact_backward_f32(ExactParams p, int heads_at_once) {
+  extern __shared__ __align__(16) char smem[];
+  const int nkt = (p.nk + 31) / 32, keys = nkt * p.Hk * p.B * p.kv_splits;
+  int bid = blockIdx.x;
+  if (bid < keys) {
+    const int kt = bid % nkt;
+    bid /= nkt;
+    const int hk = bid % p.Hk;
+    bid /= p.Hk;
+    const int64_t part = ((int64_t)bid * nkt + kt) * kExWaves;  // bid: split * B + batch row
+    ex_dkv_block<float, BIAS, 1, kExWaves, false>(p, smem, kt, hk, bid % p.B, bid / p.B, p.kv_splits, part, heads_at_once);
+  } else {
+    bid -= keys;
+    const int nvt = (int)((p.nq * p.Gp + 31) / 32), Hx = p.H / p.Gp, at = bid / nvt;
+    ex_dq_block<float, BIAS, 1, kExWaves, false>(p, smem, bid % nvt, at % Hx, at / Hx, p.Gp);
+  }
 }
 
 // ------------------------------------------------------------------ tiles of 64 rows, bf16
@@ -715,7 +766,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   wait_vmcnt<0>();  // no load is under way into what is written next
   __syncthreads();
   if (WIN && qw == global) return;  // another block has these rows
-  if (hf == 0 && i < p.nq) ex_put_stat<uint16_t>(p, ((int64_t)b * p.H + h) * p.nq + i, cr, D);
+  if (hf == 0 && i < p.nq) ex_put_stat(p, ((int64_t)b * p.H + h) * p.nq + i, cr, D);
   char* out = static_cast<char*>(p.dQ.data) + (b * p.dQ.batch + (int64_t)qw * p.dQ.row + hcol) * 2;
   ex_store_rows32(smem + wave * 32 * 144, dq, p.scale, out, p.dQ.row * 2, p.nq - qw, lane);
 }
@@ -1182,84 +1233,102 @@ int dkv_waves(const ExactParams& p) {  // of k_exact_dkv
 
 // The largest table (and a wave's sums along diagonals, as long) fits beside the tiles.
 constexpr size_t kMaxTable = (2 * kMaxBiasDistance + 129) * 4;
-static_assert(kDkvLds<float, 2, 4> + 5 * kMaxTable <= kMaxLds && kDkvLds<uint16_t, 2, 4> + 5 * kMaxTable <= kMaxLds &&
-              kDkvLds<uint16_t, 2, 8> + 9 * kMaxTable <= kMaxLds &&
-              kDkvTilesLds + 5 * kMaxTable <= kMaxLds / 2, "LDS of a block");
+static_assert(kDkvLds<float, 1, 4> + 5 * kMaxTable <= kMaxLds && kDkvLds<uint16_t, 2, 4> + 5 * kMaxTable <= kMaxLds &&
+              kDkvLds<uint16_t, 2, 8> + 9 * kMaxTable <= kMaxLds && kDkvTilesLds + 5 * kMaxTable <= kMaxLds / 2, "LDS of a block");
 
-template <typename T, bool BIAS, int ST, int W, bool FEW = false>
+template <bool BIAS>
+size_t table_bytes(const ExactParams& p) { return BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0; }
+
+template <bool BIAS, int W, bool FEW>
 hipError_t launch_dq_of(const ExactParams& p, hipStream_t s) {
-  const size_t lds = kDqLds<T, ST, W> + (BIAS ? (size_t)p.Gp * exact_bias_entries(p.D) * 4 : 0);
-  const hipError_t e = exact_set_lds<k_exact_dq<T, BIAS, ST, W, FEW>>(lds);
+  const size_t lds = kDqLds<uint16_t, 2, W> + table_bytes<BIAS>(p) * p.Gp;
+  const hipError_t e = exact_set_lds<k_exact_dq<BIAS, W, FEW>>(lds);
   if (e != hipSuccess) return e;
   const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B;
-  hipLaunchKernelGGL((k_exact_dq<T, BIAS, ST, W, FEW>), dim3((unsigned)blocks), dim3(64 * W), lds, s, p);
+  hipLaunchKernelGGL((k_exact_dq<BIAS, W, FEW>), dim3((unsigned)blocks), dim3(64 * W), lds, s, p);
   return hipGetLastError();
 }
 
-template <typename T, bool BIAS>
+template <bool BIAS>
 hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
-  if constexpr (ExFmt<T>::ES == 2) {
-    if (dq_in_tiles(p)) {
-      const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
-      const int64_t blocks = (int64_t)((p.nq + 127) / 128) * p.H * p.B;
-      if (p.window && !p.causal) {
-        const size_t lds = kDqLds<T, 2, 4> + table;
-        const hipError_t e =  exact_set_lds<k_exact_dq_tiles<BIAS, true>>(lds);
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, true>), dim3((unsigned)(blocks + p.H * p.B)), dim3(kExThreads), lds, s, p);
-      } else {
-        hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, false>), dim3((unsigned)blocks), dim3(kExThreads), 6 * kTile64 + table, s, p);
-      }
-      return hipGetLastError();
-    }
+  if (!dq_in_tiles(p)) {
+    if (few(p)) return launch_dq_of<BIAS, 4, true>(p, s);
+    return exact_eight_waves(exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B, (p.nk + 31) / 32) ? launch_dq_of<BIAS, 8, false>(p, s)
+                                                                                                : launch_dq_of<BIAS, 4, false>(p, s);
   }
-  const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B, tiles = (p.nk + 31) / 32;
-  if constexpr (ExFmt<T>::ES == 4) {  // as the forward pass
-    if (blocks > device_cus()) return launch_dq_of<T, BIAS, 1, 4>(p, s);
+  const int64_t blocks = (int64_t)((p.nq + 127) / 128) * p.H * p.B;
+  if (p.window && !p.causal) {
+    const size_t lds = kDqLds<uint16_t, 2, 4> + table_bytes<BIAS>(p);
+    const hipError_t e = exact_set_lds<k_exact_dq_tiles<BIAS, true>>(lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, true>), dim3((unsigned)(blocks + p.H * p.B)), dim3(kExThreads), lds, s, p);
   } else {
-    if (few(p)) return launch_dq_of<T, BIAS, 2, 4, true>(p, s);
-    if (exact_eight_waves(blocks, tiles)) return launch_dq_of<T, BIAS, 2, 8>(p, s);
+    hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, false>), dim3((unsigned)blocks), dim3(kExThreads), 6 * kTile64 + table_bytes<BIAS>(p), s, p);
   }
-  return launch_dq_of<T, BIAS, 2, 4>(p, s);
+  return hipGetLastError();
 }
 
-// A block's tiles and its waves' sums along diagonals in LDS, then the bias tables of as many heads as fit.
+// A block's tiles and its waves' sums along diagonals in LDS, then the bias tables of as many heads as fit. `blocks`
+// of it, that need `least` LDS.
 template <auto K, bool BIAS, int W = kExWaves>
-hipError_t launch_dkv_kernel(const ExactParams& p, int keys, size_t base, hipStream_t s, int more = 0) {
-  const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
+hipError_t launch_dkv_kernel(const ExactParams& p, int64_t blocks, size_t base, hipStream_t s, size_t least = 0) {
+  const size_t table = table_bytes<BIAS>(p);
   base += W * table;
   int heads = p.G;
   if constexpr (BIAS) {
-    const size_t room = base + table <= kMaxLds / 2 ? kMaxLds / 2 : kMaxLds;  // two blocks to a CU, or one
+    const size_t room = std::max(base + table, least) <= kMaxLds / 2 ? kMaxLds / 2 : kMaxLds;  // two blocks to a CU, or one
     heads = (int)std::min<size_t>(heads, (room - base) / table);
   }
-  const size_t lds = base + table * heads;
+  const size_t lds = std::max(base + table * heads, least);
   const hipError_t e = exact_set_lds<K>(lds);
   if (e != hipSuccess) return e;
-  const int64_t blocks = (int64_t)((p.nk + keys - 1) / keys) * p.Hk * p.B * p.kv_splits + more;
   hipLaunchKernelGGL(K, dim3((unsigned)blocks), dim3(64 * W), lds, s, p, heads);
   return hipGetLastError();
 }
+// Blocks of `keys` keys.
+int64_t dkv_blocks(const ExactParams& p, int keys) { return (int64_t)((p.nk + keys - 1) / keys) * p.Hk * p.B * p.kv_splits; }
 
-template <typename T, bool BIAS, int ST, int W, bool FEW = false>
+template <bool BIAS, int W, bool FEW>
 hipError_t launch_dkv_of(const ExactParams& p, hipStream_t s) {
-  return launch_dkv_kernel<k_exact_dkv<T, BIAS, ST, W, FEW>, BIAS, W>(p, 32, kDkvLds<T, ST, W>, s);
+  return launch_dkv_kernel<k_exact_dkv<BIAS, W, FEW>, BIAS, W>(p, dkv_blocks(p, 32), kDkvLds<uint16_t, 2, W>, s);
+}
+template <bool BIAS>
+hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
+  if (!dkv_in_tiles(p)) {
+    if (few(p)) return launch_dkv_of<BIAS, 4, true>(p, s);
+    return dkv_waves(p) == 8 ? launch_dkv_of<BIAS, 8, false>(p, s) : launch_dkv_of<BIAS, 4, false>(p, s);
+  }
+  const int64_t blocks = dkv_blocks(p, 128);
+  if (p.window)
+    return launch_dkv_kernel<k_exact_dkv_tiles<BIAS, true>, BIAS>(p, blocks + (int64_t)p.Hk * p.B, kDkvLds<uint16_t, 2, 4>, s);
+  return launch_dkv_kernel<k_exact_dkv_tiles<BIAS, false>, BIAS>(p, blocks, kDkvTilesLds, s);
+}
+
+template <bool BIAS>
+hipError_t launch_f32(const ExactParams& p, hipStream_t s) {
+  const int64_t rows = ((int64_t)p.B * p.nq * p.H + kExThreads / 16 - 1) / (kExThreads / 16);
+  hipLaunchKernelGGL(k_exact_stats, dim3((unsigned)rows), dim3(kExThreads), 0, s, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_dkv_kernel<k_exact_backward_f32<BIAS>, BIAS>(p, dkv_blocks(p, 32) + exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B,
+                                                            kDkvLds<float, 1, 4>, s, kDqLds<float, 1, 4> + table_bytes<BIAS>(p) * p.Gp);
 }
 
 template <typename T, bool BIAS>
-hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
-  hipError_t e = hipErrorInvalidValue;
-  if (!dkv_in_tiles(p)) {
-    const int64_t blocks = (int64_t)((p.nk + 31) / 32) * p.Hk * p.B * p.kv_splits;
-    if constexpr (ExFmt<T>::ES == 4) {  // as the forward pass
-      e = blocks > device_cus() ? launch_dkv_of<T, BIAS, 1, 4>(p, s) : launch_dkv_of<T, BIAS, 2, 4>(p, s);
-    } else {
-      e = few(p) ? launch_dkv_of<T, BIAS, 2, 4, true>(p, s)
-                 : dkv_waves(p) == 8 ? launch_dkv_of<T, BIAS, 2, 8>(p, s) : launch_dkv_of<T, BIAS, 2, 4>(p, s);
+hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
+  hipError_t e;
+  if constexpr (ExFmt<T>::ES == 2) {
+    if (!BIAS && exact_backward_small(p)) {
+      const bool f = few(p);
+      e = f ? exact_set_lds<k_exact_backward_small<true>>(kSmallLds) : exact_set_lds<k_exact_backward_small<false>>(kSmallLds);
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(f ? k_exact_backward_small<true> : k_exact_backward_small<false>, dim3((unsigned)(p.H * p.B)),
+                         dim3(kExThreads), kSmallLds, s, p);
+      return hipGetLastError();
     }
-  } else if constexpr (ExFmt<T>::ES == 2) {
-    if (p.window) e = launch_dkv_kernel<k_exact_dkv_tiles<BIAS, true>, BIAS>(p, 128, kDkvLds<T, 2, 4>, s, p.Hk * p.B);
-    else e = launch_dkv_kernel<k_exact_dkv_tiles<BIAS, false>, BIAS>(p, 128, kDkvTilesLds, s);
+    if ((e = launch_dq<BIAS>(p, s)) == hipSuccess) e = launch_dkv<BIAS>(p, s);
+  } else {
+    e = launch_f32<BIAS>(p, s);
   }
   if (e != hipSuccess) return e;
   const int sums = BIAS ? (p.buckets * p.H + kExWaves - 1) / kExWaves : 0;
@@ -1267,22 +1336,6 @@ hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
   if (sums + rows == 0) return hipSuccess;
   hipLaunchKernelGGL((k_exact_join_grads<T>), dim3((unsigned)(sums + rows)), dim3(kExThreads), 0, s, p, sums);
   return hipGetLastError();
-}
-
-template <typename T, bool BIAS>
-hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
-  if constexpr (ExFmt<T>::ES == 2 && !BIAS) {
-    if (exact_backward_small(p)) {
-      const bool f = few(p);
-      const hipError_t e = f ? exact_set_lds<k_exact_backward_small<true>>(kSmallLds) : exact_set_lds<k_exact_backward_small<false>>(kSmallLds);
-      if (e != hipSuccess) return e;
-      hipLaunchKernelGGL(f ? k_exact_backward_small<true> : k_exact_backward_small<false>, dim3((unsigned)(p.H * p.B)),
-                         dim3(kExThreads), kSmallLds, s, p);
-      return hipGetLastError();
-    }
-  }
-  const hipError_t e = launch_dq<T, BIAS>(p, s);
-  return e != hipSuccess ? e : launch_dkv<T, BIAS>(p, s);
 }
 
 }  // namespace
