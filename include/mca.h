@@ -256,7 +256,7 @@ mca_status mca_attention_forward_noalloc(const mca_forward_desc* desc, const voi
  * their matrix products rounded to bfloat16 (to twice the bits in calls of few keys or
  * queries), and results are rounded once.
  * Q, K, V, dY and the bias are expected to be finite (the bias: or masking); a non-finite
- * value in an attended row makes results that depend on it unspecified.
+ * value in a row that is read makes the results of its batch row unspecified.
  *
  * Buckets of a relative position r = j - p (a learned bias that distinguishes near distances
  * one by one and far ones in ranges that grow): n = bias_buckets, d = max(-r, 0); or, when
