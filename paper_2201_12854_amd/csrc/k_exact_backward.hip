@@ -1040,24 +1040,17 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
 // mostly their starts and loads (backward pass, 12 heads, two launches against one: 1 x 32 tokens 11.4 and 6.1
 // us; 1 x 128 11.8 and 10.4; 32 x 128 24.7 and 18.7; 128 x 128 69 and 51).
 constexpr int kSmallRows = 128;
-constexpr int kSmallLds = 4 * kSmallRows * 128 + 2 * kSmallRows * 4;  // the matrices, where S and dP start
-
-// 32 rows of a lane's own from registers: 8 bytes to a store (the LDS is all in use).
-__device__ __forceinline__ void ex_store_lane_row(const f32x16_t (&y)[2], float scale, uint16_t* row, int hf) {
-#pragma unroll
-  for (int cc = 0; cc < 2; ++cc)
-#pragma unroll
-    for (int r = 0; r < 16; r += 4)
-      *reinterpret_cast<uint2*>(row + 32 * cc + 2 * r + 4 * hf) =
-          make_uint2(pack_bf16x2(y[cc][r] * scale, y[cc][r + 1] * scale), pack_bf16x2(y[cc][r + 2] * scale, y[cc][r + 3] * scale));
-}
+// Rows that a block has room for, 32 for each of its waves: with fewer waves more blocks are on a CU (against four
+// always: 128 x 32 tokens 13.0 and 19.9 us, 64 x 64 15.0 and 17.7, 300 x 40, 16 heads, 49 and 73).
+__host__ __device__ inline int small_rows(const ExactParams& p) { return (max(p.nq, p.nk) + 31) / 32 * 32; }
 
 template <bool FEW>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_backward_small(ExactParams p) {
   using T = uint16_t;
   extern __shared__ __align__(16) char smem[];  // Q, K, V, dY; -c / s2 and -D per query
-  char *Qs = smem, *Ks = smem + 16384, *Vs = smem + 32768, *Ys = smem + 49152;
-  float* stat = reinterpret_cast<float*>(smem + 65536);
+  const int rows = small_rows(p), M = rows * 128;
+  char *Qs = smem, *Ks = smem + M, *Vs = smem + 2 * M, *Ys = smem + 3 * M;
+  float* stat = reinterpret_cast<float*>(smem + 4 * M);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hf = lane >> 5, h = blockIdx.x % p.H, b = blockIdx.x / p.H, r0 = 32 * wave;
   const ExRow0 br = ex_batch_row(p, b);
@@ -1067,10 +1060,10 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     const char* base = static_cast<const char*>(m.data) + (b * m.batch + hcol) * 2;
     ex_load_tile<T>(ex_rsrc(base, m.row * 2, r0, limit, 128), (int)m.row * 2, to + at, lane);
   };
-  load(p.K, br.klen, 16384);
-  load(p.V, br.klen, 32768);
+  load(p.K, br.klen, M);
+  load(p.V, br.klen, 2 * M);
   load(p.Q, br.qlen, 0);
-  load(p.dY, br.qlen, 49152);
+  load(p.dY, br.qlen, 3 * M);
   const int i = r0 + c;
   float D = 0.f, cr = INFINITY;  // a row without keys, or behind the last query: every P is 0
   if (i < br.qlen) {
@@ -1124,9 +1117,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   }
   if (hf == 0) {
     stat[i] = -cr * (1.f / p.s2);
-    stat[kSmallRows + i] = -D;
+    stat[rows + i] = -D;
   }
-  if (i < p.nq) ex_store_lane_row(dq, p.scale, static_cast<T*>(p.dQ.data) + b * p.dQ.batch + i * p.dQ.row + hcol, hf);
   __syncthreads();
 
   f32x16_t dk[2] = {ex_zero16(), ex_zero16()}, dv[2] = {ex_zero16(), ex_zero16()};
@@ -1148,7 +1140,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
 #pragma unroll
       for (int k = 0; k < 4; ++k) {  // rows 8 k + 4 hf ..
         const float4 u = *reinterpret_cast<const float4*>(stat + i0 + 8 * k + 4 * hf);
-        const float4 w = *reinterpret_cast<const float4*>(stat + kSmallRows + i0 + 8 * k + 4 * hf);
+        const float4 w = *reinterpret_cast<const float4*>(stat + rows + i0 + 8 * k + 4 * hf);
         x[4 * k] += u.x, x[4 * k + 1] += u.y, x[4 * k + 2] += u.z, x[4 * k + 3] += u.w;
         ds[4 * k] += w.x, ds[4 * k + 1] += w.y, ds[4 * k + 2] += w.z, ds[4 * k + 3] += w.w;
       }
@@ -1166,7 +1158,9 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   __syncthreads();
   if (i >= br.klen) dk[0] = dk[1] = dv[0] = dv[1] = ex_zero16();
   char* st = smem + wave * 32 * 144;
-  char* out = static_cast<char*>(p.dK.data) + (b * p.dK.batch + (int64_t)r0 * p.dK.row + hcol) * 2;
+  char* out = static_cast<char*>(p.dQ.data) + (b * p.dQ.batch + (int64_t)r0 * p.dQ.row + hcol) * 2;
+  ex_store_rows32(st, dq, p.scale, out, p.dQ.row * 2, p.nq - r0, lane);
+  out = static_cast<char*>(p.dK.data) + (b * p.dK.batch + (int64_t)r0 * p.dK.row + hcol) * 2;
   ex_store_rows32(st, dk, p.scale, out, p.dK.row * 2, p.nk - r0, lane);
   out = static_cast<char*>(p.dV.data) + (b * p.dV.batch + (int64_t)r0 * p.dV.row + hcol) * 2;
   ex_store_rows32(st, dv, 1.f, out, p.dV.row * 2, p.nk - r0, lane);
@@ -1319,11 +1313,12 @@ hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
   hipError_t e;
   if constexpr (ExFmt<T>::ES == 2) {
     if (!BIAS && exact_backward_small(p)) {
+      const int rows = small_rows(p), lds = rows * (4 * 128 + 8);  // the matrices, where S and dP start
       const bool f = few(p);
-      e = f ? exact_set_lds<k_exact_backward_small<true>>(kSmallLds) : exact_set_lds<k_exact_backward_small<false>>(kSmallLds);
+      e = f ? exact_set_lds<k_exact_backward_small<true>>(lds) : exact_set_lds<k_exact_backward_small<false>>(lds);
       if (e != hipSuccess) return e;
       hipLaunchKernelGGL(f ? k_exact_backward_small<true> : k_exact_backward_small<false>, dim3((unsigned)(p.H * p.B)),
-                         dim3(kExThreads), kSmallLds, s, p);
+                         dim3(2 * rows), lds, s, p);
       return hipGetLastError();
     }
     if ((e = launch_dq<BIAS>(p, s)) == hipSuccess) e = launch_dkv<BIAS>(p, s);
