@@ -56,6 +56,17 @@ inline int exact_bias_entries(int D) { return 2 * D + 129; }  // rel = j - p in 
 // Rows (query, head) that the kernels of 32 rows pad to.
 inline int64_t exact_row_tiles(int64_t nq, int64_t Gp) { return (nq * Gp + 31) / 32; }
 
+// Calls whose (batch row, head)s fit a block each: bf16, at most so many queries and keys. The backward pass is
+// one launch then, without a workspace.
+constexpr int kSmallRows = 128;
+inline bool exact_small(const ExactParams& p) {
+  return p.bf16 && !p.table && p.nq <= kSmallRows && p.nk <= kSmallRows && p.G == 1;
+}
+// Rows that such a block has room for, 32 for each of its waves: with fewer waves more blocks are on a CU
+// (backward pass, against four always: 128 x 32 tokens, 12 heads, 13.0 and 19.9 us, 64 x 64 15.0 and 17.7, 300 x
+// 40, 16 heads, 49 and 73).
+__host__ __device__ inline int exact_small_rows(const ExactParams& p) { return ((p.nq > p.nk ? p.nq : p.nk) + 31) / 32 * 32; }
+
 constexpr size_t kMaxLds = 163840;  // of a block: a CU's
 
 // Allows kernel K that much LDS less STATIC of its own, once per device; an error where `lds` is more.
@@ -80,7 +91,6 @@ inline bool exact_worth(int64_t tiles, int64_t n, int unit) {
 bool exact_eight_waves(int64_t blocks, int64_t tiles);  // of the kernels of 32 rows, for a block's tiles
 int exact_splits(const ExactParams& p);
 int exact_kv_splits(const ExactParams& p);
-bool exact_backward_small(const ExactParams& p);  // in one launch, without a workspace
 int64_t exact_bias_parts(const ExactParams& p);
 int exact_group(const ExactParams& p);  // Gp
 hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s);

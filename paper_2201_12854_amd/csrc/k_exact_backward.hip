@@ -1039,16 +1039,11 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
 // take 32 queries each for D and dQ, and then 32 keys each for dK and dV. What two launches cost at this size is
 // mostly their starts and loads (backward pass, 12 heads, two launches against one: 1 x 32 tokens 11.4 and 6.1
 // us; 1 x 128 11.8 and 10.4; 32 x 128 24.7 and 18.7; 128 x 128 69 and 51).
-constexpr int kSmallRows = 128;
-// Rows that a block has room for, 32 for each of its waves: with fewer waves more blocks are on a CU (against four
-// always: 128 x 32 tokens 13.0 and 19.9 us, 64 x 64 15.0 and 17.7, 300 x 40, 16 heads, 49 and 73).
-__host__ __device__ inline int small_rows(const ExactParams& p) { return (max(p.nq, p.nk) + 31) / 32 * 32; }
-
 template <bool FEW>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_backward_small(ExactParams p) {
   using T = uint16_t;
   extern __shared__ __align__(16) char smem[];  // Q, K, V, dY; -c / s2 and -D per query
-  const int rows = small_rows(p), M = rows * 128;
+  const int rows = exact_small_rows(p), M = rows * 128;
   char *Qs = smem, *Ks = smem + M, *Vs = smem + 2 * M, *Ys = smem + 3 * M;
   float* stat = reinterpret_cast<float*>(smem + 4 * M);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1312,8 +1307,8 @@ template <typename T, bool BIAS>
 hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
   hipError_t e;
   if constexpr (ExFmt<T>::ES == 2) {
-    if (!BIAS && exact_backward_small(p)) {
-      const int rows = small_rows(p), lds = rows * (4 * 128 + 8);  // the matrices, where S and dP start
+    if (!BIAS && exact_small(p)) {
+      const int rows = exact_small_rows(p), lds = rows * (4 * 128 + 8);  // the matrices, where S and dP start
       const bool f = few(p);
       e = f ? exact_set_lds<k_exact_backward_small<true>>(lds) : exact_set_lds<k_exact_backward_small<false>>(lds);
       if (e != hipSuccess) return e;
@@ -1335,16 +1330,12 @@ hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
 
 }  // namespace
 
-bool exact_backward_small(const ExactParams& p) {
-  return p.bf16 && !p.table && p.nq <= kSmallRows && p.nk <= kSmallRows && p.G == 1;
-}
-
 // Blocks that share a key's queries: where they leave CUs without one (few keys, or few key heads with
 // many query heads), as many as that takes, of sixteen tiles of 64 at least, or a tile of 32 to a wave
 // where that saves more than the join takes.
 int exact_kv_splits(const ExactParams& p) {
   const bool big = dkv_in_tiles(p);
-  if ((big && p.window) || exact_backward_small(p)) return 1;
+  if ((big && p.window) || exact_small(p)) return 1;
   const int64_t blocks = (int64_t)((p.nk + (big ? 127 : 31)) / (big ? 128 : 32)) * p.Hk * p.B;
   const int64_t tiles = (int64_t)p.G * ((p.nq + (big ? 63 : 31)) / (big ? 64 : 32));
   const int64_t n = std::min((big ? 2 : 1) * device_cus() / blocks, tiles / (big ? 16 : kExWaves));

@@ -222,6 +222,59 @@ __global__ __launch_bounds__(kExThreads) void k_exact_join(ExactParams p) {
   if (lane == 0) p.lse[((int64_t)b * p.H + h) * p.nq + i] = L > 0.f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
 }
 
+// ------------------------------------------------------------------ up to 128 queries and keys, bf16
+// For grids that fill the card: a block has a (batch row, head)'s K and V in LDS, a wave 32 of its queries. Bound
+// by memory where there are many (128 x 128 tokens, 12 heads, 19.5 us for 101 MB; in blocks of 128 queries
+// 21.6); a wave for each 32 rows puts more short rows on a CU (300 x 40, 16 heads, 19 and 33 us; 64 x 64 6.5
+// and 8.0; 64 rows of 16 to 128 10.6 and 10.9).
+__global__ __launch_bounds__(kExThreads) void k_exact_forward_small(ExactParams p) {
+  using T = uint16_t;
+  extern __shared__ __align__(16) char smem[];  // K, V
+  const int M = exact_small_rows(p) * 128;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, hf = lane >> 5, h = blockIdx.x % p.H, b = blockIdx.x / p.H, r0 = 32 * wave, i = r0 + c;
+  const ExRow0 br = ex_batch_row(p, b);
+  const int64_t hcol = h * kDHead;
+  auto load = [&](const ExactRows& m, uint32_t to) __attribute__((always_inline)) {
+    const char* base = static_cast<const char*>(m.data) + (b * m.batch + hcol) * 2;
+    ex_load_tile<T>(ex_rsrc(base, m.row * 2, r0, br.klen, 128), (int)m.row * 2, lds_addr(smem) + to + 4096u * wave, lane);
+  };
+  load(p.K, 0);
+  load(p.V, M);
+  const char* qrow = static_cast<const char*>(p.Q.data) + (b * p.Q.batch + i * p.Q.row + hcol) * 2;
+  const ExRow<T> q = i < br.qlen ? ex_global_row<T>(qrow, hf) : ex_zero_row<T>();
+  wait_vmcnt<0>();
+  __syncthreads();
+
+  ExState s;
+  s.m = -INFINITY;
+  s.l = 0.f;
+  s.y[0] = s.y[1] = ex_zero16();
+  const int last = min(r0 + 32, br.qlen) - 1;
+  if (last >= r0) {  // wave-uniform
+    const ExTiles tiles = ex_key_tiles(p, br.pos + r0, br.pos + last, br.klen);
+    const ExSpan keys = ex_keys_of(p, br.pos + i, br.klen);
+#pragma clang loop unroll(disable)
+    for (int t = 0; t < tiles.n; ++t) {
+      const int kt = ex_tile_at(tiles, t), k0 = 32 * kt;
+      f32x16_t x = ex_rows_product<T>(smem + 4096 * kt, q, c, hf);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] *= p.s2;
+      if (!ex_whole(p, br.pos + r0, br.pos + last, k0, br.klen)) ex_mask(x, keys, k0 + 4 * hf, k0 > 0);
+      ex_softmax_step(s, x);
+      ex_cols_product<T>(s.y, smem + M + 4096 * kt, x, lane);
+    }
+  }
+  s.l += ex_other_half(s.l);
+  const float L = i < br.qlen ? s.l : 0.f;
+  if (L == 0.f) s.y[0] = s.y[1] = ex_zero16();
+  if (hf == 0 && i < p.nq)
+    p.lse[((int64_t)b * p.H + h) * p.nq + i] = L > 0.f ? (s.m + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
+  __syncthreads();
+  char* out = static_cast<char*>(p.Yo.data) + (b * p.Yo.batch + (int64_t)r0 * p.Yo.row + hcol) * 2;
+  ex_store_rows32(smem + wave * 32 * 144, s.y, L > 0.f ? 1.f / L : 0.f, out, p.Yo.row * 2, p.nq - r0, lane);
+}
+
 // ------------------------------------------------------------------ 128 or 256 queries per block, bf16
 // Four waves of 32 MT queries of one head share key tiles of 64. What bounds it is issue on each
 // SIMD, as in the output pass of the sampled layer: a half tile of 32 keys runs as slots that are
@@ -600,6 +653,11 @@ int exact_splits(const ExactParams& p) {
 bool exact_eight_waves(int64_t blocks, int64_t tiles) { return tiles > 8 && blocks <= device_cus(); }
 
 hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s) {
+  if (exact_small(p) && forward_in_tiles(p)) {
+    const int rows = exact_small_rows(p);
+    hipLaunchKernelGGL(k_exact_forward_small, dim3((unsigned)(p.H * p.B)), dim3(2 * rows), rows * 256, s, p);
+    return hipGetLastError();
+  }
   if (forward_in_tiles(p)) {
     if (p.window && !p.causal) return p.table ? launch_tiles<true, 1, true>(p, s) : launch_tiles<false, 1, true>(p, s);
     if (p.table) return launch_tiles<true, 1, false>(p, s);

@@ -71,6 +71,11 @@ SHAPES = [  # B, nq, nk, heads, kv_heads, options
     (2, 330, 330, 4, 4, dict(kv_lens=[330, 290], q_lens=[330, 289])),
     (1, 300, 289, 6, 2, dict(causal=True)),
     (1, 500, 500, 3, 3, dict(window=40)),
+    # up to 128 queries and keys, more of them than the card has CUs
+    (30, 128, 128, 12, 12, dict(kv_lens=[128, 1, 0, 33, 64, 100] * 5, q_lens=[128, 1, 40, 0, 65, 97] * 5)),
+    (60, 33, 64, 8, 8, dict(causal=True, q_pos=[0, 31, -40] * 20)),
+    (40, 70, 90, 9, 9, dict(window=20, q_pos=[0, 15, -30, 60] * 10)),
+    (300, 1, 2, 2, 2, {}),
     # up to 128 queries and keys: one launch for the gradients in bfloat16
     (3, 128, 100, 4, 4, dict(window=16, q_lens=[128, 33, 1], kv_lens=[100, 64, 2])),
     (2, 100, 128, 3, 3, dict(window=30, causal=True, q_pos=[28, -40])),
