@@ -56,12 +56,11 @@ inline int exact_bias_entries(int D) { return 2 * D + 129; }  // rel = j - p in 
 // Rows (query, head) that the kernels of 32 rows pad to.
 inline int64_t exact_row_tiles(int64_t nq, int64_t Gp) { return (nq * Gp + 31) / 32; }
 
-// Calls whose (batch row, head)s fit a block each: bf16, at most so many queries and keys. The backward pass is
-// one launch then, without a workspace.
+// Calls whose (batch row, head)s fit a block each: bf16, at most so many queries and keys. Without shared key heads
+// the backward pass is one launch then, without a workspace.
 constexpr int kSmallRows = 128;
-inline bool exact_small(const ExactParams& p) {
-  return p.bf16 && !p.table && p.nq <= kSmallRows && p.nk <= kSmallRows && p.G == 1;
-}
+inline bool exact_small(const ExactParams& p) { return p.bf16 && !p.table && p.nq <= kSmallRows && p.nk <= kSmallRows; }
+inline bool exact_backward_small(const ExactParams& p) { return exact_small(p) && p.G == 1; }
 // Rows that such a block has room for, 32 for each of its waves: with fewer waves more blocks are on a CU
 // (backward pass, against four always: 128 x 32 tokens, 12 heads, 13.0 and 19.9 us, 64 x 64 15.0 and 17.7, 300 x
 // 40, 16 heads, 49 and 73).

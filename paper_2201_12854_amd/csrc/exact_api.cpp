@@ -166,7 +166,7 @@ size_t carve(ExactParams& p, bool backward, char* ws) {
     off += align256(bytes);
     return at;
   };
-  if (backward && mca::exact_small(p)) return 0;
+  if (backward && mca::exact_backward_small(p)) return 0;
   if (backward) {
     p.rowstat = reinterpret_cast<float*>(take(8 * (size_t)p.B * p.H * p.nq));
     if (p.kv_splits > 1) {

@@ -1307,7 +1307,7 @@ template <typename T, bool BIAS>
 hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
   hipError_t e;
   if constexpr (ExFmt<T>::ES == 2) {
-    if (!BIAS && exact_small(p)) {
+    if (!BIAS && exact_backward_small(p)) {
       const int rows = exact_small_rows(p), lds = rows * (4 * 128 + 8);  // the matrices, where S and dP start
       const bool f = few(p);
       e = f ? exact_set_lds<k_exact_backward_small<true>>(lds) : exact_set_lds<k_exact_backward_small<false>>(lds);
@@ -1335,7 +1335,7 @@ hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
 // where that saves more than the join takes.
 int exact_kv_splits(const ExactParams& p) {
   const bool big = dkv_in_tiles(p);
-  if ((big && p.window) || exact_small(p)) return 1;
+  if ((big && p.window) || exact_backward_small(p)) return 1;
   const int64_t blocks = (int64_t)((p.nk + (big ? 127 : 31)) / (big ? 128 : 32)) * p.Hk * p.B;
   const int64_t tiles = (int64_t)p.G * ((p.nq + (big ? 63 : 31)) / (big ? 64 : 32));
   const int64_t n = std::min((big ? 2 : 1) * device_cus() / blocks, tiles / (big ? 16 : kExWaves));

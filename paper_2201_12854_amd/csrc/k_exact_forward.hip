@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_forward_small(ExactParams 
   const ExRow0 br = ex_batch_row(p, b);
   const int64_t hcol = h * kDHead;
   auto load = [&](const ExactRows& m, uint32_t to) __attribute__((always_inline)) {
-    const char* base = static_cast<const char*>(m.data) + (b * m.batch + hcol) * 2;
+    const char* base = static_cast<const char*>(m.data) + (b * m.batch + h / p.G * kDHead) * 2;
     ex_load_tile<T>(ex_rsrc(base, m.row * 2, r0, br.klen, 128), (int)m.row * 2, lds_addr(smem) + to + 4096u * wave, lane);
   };
   load(p.K, 0);

@@ -76,6 +76,7 @@ SHAPES = [  # B, nq, nk, heads, kv_heads, options
     (60, 33, 64, 8, 8, dict(causal=True, q_pos=[0, 31, -40] * 20)),
     (40, 70, 90, 9, 9, dict(window=20, q_pos=[0, 15, -30, 60] * 10)),
     (300, 1, 2, 2, 2, {}),
+    (40, 61, 50, 12, 3, dict(causal=True, kv_lens=[50, 7] * 20)),
     # up to 128 queries and keys: one launch for the gradients in bfloat16
     (3, 128, 100, 4, 4, dict(window=16, q_lens=[128, 33, 1], kv_lens=[100, 64, 2])),
     (2, 100, 128, 3, 3, dict(window=30, causal=True, q_pos=[28, -40])),
