@@ -1201,9 +1201,8 @@ __global__ __launch_bounds__(kExThreads) void k_exact_join_grads(ExactParams p, 
 }
 
 // bf16 in blocks of 128 rows where the blocks of 32 are more than the CUs, or, in a long loop, which is all a
-// block of 128 has on a CU then, twice as many (backward pass, 12 heads: 8 x 128 tokens, 384 blocks of 32,
-// 16.7 against 14.8 us; 4 x 256 22.4 and 18.6; 2 x 512 26.1 and 31.9; 1 x 1024 34.4 and 44.1; 2 x 256, 192
-// blocks, 13.5 and 18.2).
+// block of 128 has on a CU then, twice as many (backward pass, 12 heads: 4 x 256 tokens, 384 blocks of 32,
+// 22.4 against 18.6 us; 2 x 512 26.1 and 31.9; 1 x 1024 34.4 and 44.1; 2 x 256, 192 blocks, 13.5 and 18.2).
 bool in_tiles(const ExactParams& p, int64_t blocks, int loop) {
   return p.bf16 && blocks > (loop > 384 ? 2 : 1) * (int64_t)device_cus();
 }

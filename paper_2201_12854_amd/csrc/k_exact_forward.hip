@@ -611,9 +611,9 @@ int exact_group(const ExactParams& p) {
   return !p.table || (int64_t)p.G * exact_bias_entries(p.D) * 4 <= (int64_t)kMaxLds - kRowLds<float, 2, 4> ? p.G : 1;
 }
 
-// bf16 in blocks of 128 queries or more: where the blocks of 32 rows are more than the CUs (forward, 12
-// heads: 8 x 128 tokens, 384 blocks of 32, 6.9 against 6.3 us; 16 x 64 6.6 and 5.4; 1 x 1024 23.8 and 16.6;
-// 2 x 256, 192 blocks, 6.1 and 7.8; 1 x 512 7.5 and 10.5). Rows of a single block of 32 over many keys
+// bf16 in blocks of 128 queries or more, or of a whole short row: where the blocks of 32 rows are more than the CUs
+// (forward, 12 heads: 8 x 128 tokens, 384 blocks of 32, 6.9 against 5.7 us; 1 x 1024 23.8 and 16.6; 2 x 256, 192
+// blocks, 6.1 and 7.8; 1 x 512 7.5 and 10.5). Rows of a single block of 32 over many keys
 // stay: its four waves share the keys, of which a wave of the other kernel reads all.
 static bool forward_in_tiles(const ExactParams& p) {
   return p.bf16 && exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B > device_cus() &&
