@@ -436,6 +436,7 @@ class _ExactCall:
     def __init__(self, Q, K, V, heads, kv_heads, scale, q_lens, kv_lens, q_pos, causal, window, bias):
         import torch
 
+        self.torch = torch
         if not Q.is_cuda or Q.dim() != 3 or K.dim() != 3 or V.dim() != 3:
             raise ValueError("Q, K and V must be 3-D device tensors")
         kv_heads = heads if kv_heads is None else kv_heads
@@ -464,16 +465,17 @@ class _ExactCall:
     def rows(self, name, t, shape) -> Rows:
         return _exact_rows(name, t, shape, self.dtype, self.device)
 
-    def check_lse(self, lse):
-        import torch
+    def new_rows(self, shape):
+        """A new tensor and its rows."""
+        t = self.new(shape)
+        return t, Rows(t.data_ptr(), shape[1] * shape[2], shape[2])
 
-        if lse.dtype != torch.float32 or lse.shape != self.lse_shape or lse.device != self.device or not lse.is_contiguous():
+    def check_lse(self, lse):
+        if lse.dtype != self.torch.float32 or lse.shape != self.lse_shape or lse.device != self.device or not lse.is_contiguous():
             raise ValueError(f"lse must be contiguous float32 {list(self.lse_shape)} on {self.device}")
         return lse
 
     def workspace(self, backward: bool, given=None):
-        import torch
-
         out = ctypes.c_size_t(0)
         _check(load_library().mca_exact_workspace_size(ctypes.byref(self.desc), int(backward), ctypes.byref(out)),
                "mca_exact_workspace_size")
@@ -481,22 +483,19 @@ class _ExactCall:
             if given.device != self.device or not given.is_contiguous():
                 raise ValueError(f"workspace must be a contiguous tensor on {self.device}")
             return given
-        return torch.empty(out.value, dtype=torch.uint8, device=self.device) if out.value else None
+        return self.new((out.value + 3) // 4, self.torch.float32) if out.value else None
 
     def new(self, shape, dtype=None):
-        import torch
-
-        return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
+        return self._keep[0].new_empty(shape, dtype=dtype or self.dtype)
 
     def run(self, fn, name, args):
         """fn(*args, stream) on the current stream of the tensors' device, with that device current."""
-        import torch
-
-        if torch.cuda.current_device() == self.device.index:
-            st = fn(*args, torch.cuda.current_stream(self.device).cuda_stream)
+        cuda = self.torch.cuda
+        if cuda.current_device() == self.device.index:
+            st = fn(*args, cuda.current_stream().cuda_stream)
         else:
-            with torch.cuda.device(self.device):
-                st = fn(*args, torch.cuda.current_stream(self.device).cuda_stream)
+            with cuda.device(self.device):
+                st = fn(*args, cuda.current_stream().cuda_stream)
         if st != MCA_OK:
             _check(st, name)
 
@@ -522,14 +521,15 @@ def exact_attention_forward(Q, K, V, *, heads: int, kv_heads: Optional[int] = No
     Returns Y [B, n_q, heads*64] of Q's dtype and lse [B, heads, n_q] float32 (-inf where a query
     attends no key; its Y is 0).
     """
-    import torch
-
     lib = load_library()
     call = _ExactCall(Q, K, V, heads, kv_heads, scale, q_lens, kv_lens, q_pos, causal, window, bias)
     ws = call.workspace(False, workspace)
-    Y, lse = out if out is not None else (call.new(call.q_shape), call.new(call.lse_shape, torch.float32))
-    y = call.rows("Y", Y, call.q_shape)
-    call.check_lse(lse)
+    if out is None:
+        (Y, y), lse = call.new_rows(call.q_shape), call.new(call.lse_shape, call.torch.float32)
+    else:
+        Y, lse = out
+        y = call.rows("Y", Y, call.q_shape)
+        call.check_lse(lse)
     call.run(lib.mca_exact_attention_forward, "mca_exact_attention_forward",
              (call.desc, call.q, call.k, call.v, y, _ptr(lse), _ptr(ws), _bytes(ws)))
     return ExactResult(Y, lse)
@@ -545,12 +545,13 @@ def exact_attention_backward(dY, Q, K, V, Y, lse, *, heads: int, kv_heads: Optio
     lib = load_library()
     call = _ExactCall(Q, K, V, heads, kv_heads, scale, q_lens, kv_lens, q_pos, causal, window, bias)
     ws = call.workspace(True, workspace)
+    dy, y = call.rows("dY", dY, call.q_shape), call.rows("Y", Y, call.q_shape)
     if out is None:
-        out = (call.new(call.q_shape), call.new(call.k_shape), call.new(call.k_shape),
-               None if bias is None else call.new(bias.table.shape))
-    dQ, dK, dV, dbias = out
-    dy, y, dq = (call.rows(n, t, call.q_shape) for n, t in (("dY", dY), ("Y", Y), ("dQ", dQ)))
-    dk, dv = (call.rows(n, t, call.k_shape) for n, t in (("dK", dK), ("dV", dV)))
+        (dQ, dq), (dK, dk), (dV, dv) = call.new_rows(call.q_shape), call.new_rows(call.k_shape), call.new_rows(call.k_shape)
+        dbias = None if bias is None else call.new(bias.table.shape)
+    else:
+        dQ, dK, dV, dbias = out
+        dq, dk, dv = (call.rows(n, t, s) for n, t, s in (("dQ", dQ, call.q_shape), ("dK", dK, call.k_shape), ("dV", dV, call.k_shape)))
     call.check_lse(lse)
     if (bias is None) != (dbias is None) or dbias is not None and (
             dbias.shape != bias.table.shape or dbias.dtype != Q.dtype or dbias.device != Q.device or not dbias.is_contiguous()):
