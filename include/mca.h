@@ -299,9 +299,9 @@ typedef struct mca_rows {
 } mca_rows;
 
 /*
- * Bytes of device workspace of mca_exact_attention_forward (backward = 0; may be 0) or
- * mca_exact_attention_backward (backward = 1) for `desc` (host only). Errors: as their
- * checks of desc.
+ * Bytes of device workspace of mca_exact_attention_forward (backward = 0) or
+ * mca_exact_attention_backward (backward = 1) for `desc` (host only); may be 0. Errors: as
+ * their checks of desc.
  */
 mca_status mca_exact_workspace_size(const mca_exact_desc* desc, int backward, size_t* bytes);
 
@@ -320,8 +320,8 @@ mca_status mca_exact_attention_forward(const mca_exact_desc* desc, const mca_row
 /*
  * Gradients of exact attention: dQ, dK, dV and, when desc has a bias table, dbias_table
  * [bias_buckets, H] (`dtype`; NULL otherwise). The values are written, not added to. Q, K, V,
- * the lengths and the bias as in the forward call that gave Y and lse. Errors: as
- * mca_exact_attention_forward.
+ * the lengths and the bias as in the forward call that gave Y and lse. `workspace` and errors:
+ * as mca_exact_attention_forward.
  */
 mca_status mca_exact_attention_backward(const mca_exact_desc* desc, const mca_rows* dY, const mca_rows* Q,
                                         const mca_rows* K, const mca_rows* V, const mca_rows* Y, const float* lse,

@@ -70,6 +70,10 @@ def test_workspace_sizes():
     assert st == binding.MCA_OK and with_bias > n
     st, few = _size(_desc(q_len=1, kv_len=16384), 0)
     assert st == binding.MCA_OK and few > 0
+    short = dict(dtype=binding.MCA_BF16, q_len=128, kv_len=128, heads=12)
+    assert _size(_desc(kv_heads=12, **short), 1) == (binding.MCA_OK, 0)  # one launch
+    for more in (dict(kv_heads=4), dict(kv_heads=12, kv_len=129), dict(kv_heads=12, dtype=binding.MCA_F32)):
+        assert _size(_desc(**dict(short, **more)), 1)[1] > 0
 
 
 REFUSED = [dict(batch=0), dict(q_len=0), dict(kv_len=0), dict(heads=0), dict(kv_heads=0), dict(kv_heads=5), dict(kv_heads=24),
