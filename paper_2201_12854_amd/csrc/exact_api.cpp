@@ -162,7 +162,7 @@ ExactParams params_of(const mca_exact_desc& d, bool backward) {
 size_t carve(ExactParams& p, bool backward, char* ws) {
   size_t off = 0;
   auto take = [&](size_t bytes) {
-    char* at = ws + off;
+    char* at = ws ? ws + off : nullptr;  // null: only the size is asked for
     off += align256(bytes);
     return at;
   };
