@@ -827,7 +827,10 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     }
   };
   const bool mine = !WIN || kw > 0;  // another block has the first 32 keys
-  const ExRange whole = ex_whole_queries(p, kw, !mine ? 0 : BIAS ? br.klen : 0x7fffffff);
+  ExRange whole = ex_whole_queries(p, kw, !mine ? 0 : BIAS ? br.klen : 0x7fffffff);
+  // rows past the last query come as zeros, scores and offsets too: under a bias their P is what exp makes of the
+  // bias alone, which may pass float32's range (without one it is 1, times zeros)
+  if constexpr (BIAS) whole.hi = min(whole.hi, br.pos + br.qlen - 32);
   const ExRange many = ex_many_keys(p, br.klen);
   float fac = p.s2, add = 0.f, far_l = 0.f, far_r = 0.f;
   int side = 0, entry = 0;  // where the half tile lies, and the entry of its first key and query
@@ -863,7 +866,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
         for (int r = 0; r < 16; ++r) s[r] = __fmaf_rn(s[r], p.s2, bv[r]);
       }
     }
-    // rows past the last query add nothing, and keys past the last key only to the bias gradient
+    // without a bias rows past the last query add nothing, and keys past the last key nothing that is stored
     if (__builtin_expect(!ex_has(whole, q0), 0)) {
       const ExSpan queries = mine ? ex_queries_of(p, br, kw + ex_opaque(c)) : ex_span(0, -1, -1);
       ex_mask(s, queries, i0 + 4 * hf, q0 > 0);
