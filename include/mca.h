@@ -255,8 +255,11 @@ mca_status mca_attention_forward_noalloc(const mca_forward_desc* desc, const voi
  * Logits, softmax statistics and all sums are float32; with bfloat16 inputs P and dS enter
  * their matrix products rounded to bfloat16 (to twice the bits in calls of few keys or
  * queries), and results are rounded once.
- * Q, K, V, dY and the bias are expected to be finite (the bias: or masking); a non-finite
- * value in a row that is read makes the results of its batch row unspecified.
+ * Q, K, V, dY and the bias are expected to be finite (the bias: at most 1e30, or masking); a
+ * non-finite value in a row that is read makes the results of its batch row unspecified. The
+ * backward pass takes P from lse as it is in float32, to about 2^-17 |lse| of its value: biases of
+ * thousands on all keys of a row cost its gradients their last digits, and a row whose |lse| is above
+ * 2^22 has no part in any gradient.
  *
  * Buckets of a relative position r = j - p (a learned bias that distinguishes near distances
  * one by one and far ones in ranges that grow): n = bias_buckets, d = max(-r, 0); or, when

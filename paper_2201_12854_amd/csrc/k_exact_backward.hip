@@ -49,6 +49,10 @@ __device__ __forceinline__ float4 ex_join_sums(const float* ys, int row, int col
   return make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
 }
 
+// c of a row, infinity (every P is 0) for one without keys. P is off by as much as float32 leaves of c, about |c|
+// 2^-18 (with the start of S at -c / s2 in bf16); where lse itself is only known to halves, past 2^22, it would be
+// anything up to infinity, so such a row (all its biases that large) takes no part either.
+__device__ __forceinline__ float ex_row_offset(float lse) { return fabsf(lse) > 0x1p22f ? INFINITY : lse * kLog2e; }
 // What k_exact_dkv starts from, bf16.
 __device__ __forceinline__ void ex_put_stat(const ExactParams& p, int64_t row, float c, float D) {
   p.rowstat[row] = -c * (1.f / p.s2);
@@ -66,7 +70,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_stats(ExactParams p) {
     const float4 g = *reinterpret_cast<const float4*>(static_cast<const float*>(p.dY.data) + b * p.dY.batch + i * p.dY.row + col);
     D = fmaf(y.w, g.w, fmaf(y.z, g.z, fmaf(y.y, g.y, y.x * g.x)));
     const float lse = p.lse[row];
-    c = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    c = ex_row_offset(lse);
   }
   D += dpp_f32<0xB1>(D);
   D += dpp_f32<0x4E>(D);
@@ -271,7 +275,7 @@ __device__ __forceinline__ void ex_dq_block(const ExactParams& p, char* smem, in
       const char* yrow = static_cast<const char*>(p.Y.data) + (b * p.Y.batch + i * p.Y.row + hcol) * ES;
       D = ex_row_dot<T>(dy, ex_global_row<T>(yrow, hf), D);
       const float lse = p.lse[row];
-      cr = lse == -INFINITY ? INFINITY : lse * kLog2e;
+      cr = ex_row_offset(lse);
     } else {  // k_exact_stats has been here
       cr = p.rowstat[row];
       D = p.rowstat[(int64_t)p.B * p.H * p.nq + row];
@@ -636,7 +640,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     D = ex_row_dot<uint16_t>(
         dy, ex_global_row<uint16_t>(static_cast<const char*>(p.Y.data) + (b * p.Y.batch + i * p.Y.row + hcol) * 2, hf), D);
     const float lse = p.lse[((int64_t)b * p.H + h) * p.nq + i];
-    cr = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    cr = ex_row_offset(lse);
   }
   load(1, 1);
   D += ex_other_half(D);
@@ -1069,7 +1073,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
     const char* g = static_cast<const char*>(p.dY.data) + (b * p.dY.batch + i * p.dY.row + hcol) * 2;
     D = ex_row_dot<T>(ex_global_row<T>(g, hf), ex_global_row<T>(y, hf), D);
     const float lse = p.lse[((int64_t)b * p.H + h) * p.nq + i];
-    cr = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    cr = ex_row_offset(lse);
   }
   D += ex_other_half(D);
   wait_vmcnt<0>();

@@ -5,7 +5,8 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_exact import _check, _make  # noqa: E402
+from exact_testutil import Case  # noqa: E402
+from test_gpu_exact import _check, _make, _run  # noqa: E402
 
 LARGE = [  # B, nq, nk, heads, kv_heads, options; query counts that are no multiple of 32 or 64
     (2, 50, 70, 4, 4, {}),
@@ -31,4 +32,38 @@ def test_large_bias(dtype, shape):
     t["table"][:, 1] -= 100
     t["table"][1, 2] = 200  # near keys on one side
     t["table"][3, 3] = 150  # those further than 20 tokens
+    _check(t, kw, bias)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shift", [-1e9, 1e7, -2e29])
+@pytest.mark.parametrize("shape", [LARGE[0], LARGE[1], LARGE[3], LARGE[4], LARGE[7], (64, 1, 5, 12, 12, {}), (2, 20, 20, 3, 3, {})],
+                         ids=lambda s: "-".join(map(str, s[:5])) + "".join(f",{k}" for k in s[5]))
+def test_rows_past_the_range_of_lse(dtype, shift, shape):
+    """A head that is masked by a large finite bias instead of -1e30: float32 no longer has the log-sum-exp that the
+    gradients start from. They are 0 there, not infinite, and what the other heads get of shared keys stays right."""
+    B, nq, nk, heads, kv, kw = shape
+    print(f"[case] lse past 2^22 {dtype} {shift} {shape}", flush=True)
+    t, kw, bias = _make(dtype, B, nq, nk, heads, kv, buckets=8, max_distance=20, **kw)
+    t["table"][:, 0] = shift
+    got = _run(t, kw, bias)
+    assert torch.isfinite(got["Y"]).all()
+    assert (got["dQ"][..., :64] == 0).all() and (got["dbias"][:, 0] == 0).all()
+    # the same call with that head masked altogether
+    t["table"][:, 0] = -1e30
+    case = Case(t["Q"], t["K"], t["V"], dY=t["dY"], table=t["table"], **kw, **bias)
+    got.update(Y=got["Y"].clone(), lse=got["lse"].clone())
+    got["Y"][..., :64] = 0
+    got["lse"][:, 0] = float("-inf")
+    case.check(got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", LARGE[:2] + LARGE[4:6], ids=lambda s: "-".join(map(str, s[:5])) + "".join(f",{k}" for k in s[5]))
+def test_shift_of_ten_thousand(dtype, shape):
+    B, nq, nk, heads, kv, kw = shape
+    print(f"[case] shift of 1e4 {dtype} {shape}", flush=True)
+    t, kw, bias = _make(dtype, B, nq, nk, heads, kv, buckets=8, max_distance=20, **kw)
+    t["table"][:, 0] = -10000.0
+    t["table"][:, 1] = 10000.0
     _check(t, kw, bias)
