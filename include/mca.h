@@ -277,7 +277,7 @@ typedef struct mca_exact_desc {
   int32_t dtype;     /* mca_dtype of every matrix and of the bias table */
   int32_t causal;    /* 0 or 1 */
   int64_t window;    /* 0, or an even number of keys */
-  double scale;      /* of the logits; finite and > 0 */
+  double scale;      /* of the logits; at least 2^-100, and finite in float32 */
   /* device [B] int32 or NULL: valid rows (clamped to 0 .. n_q and 0 .. n_k; NULL = all) and the
      position of each batch row's first query (clamped to +-2^26; NULL = 0). Need 4-byte
      alignment only. */

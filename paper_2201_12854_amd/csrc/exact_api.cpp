@@ -96,9 +96,9 @@ mca_status check_exact(const mca_exact_desc* d) {
   if (d->window < 0 || d->window % 2 != 0 || d->window > (int64_t(1) << 25))
     return fail(MCA_ERR_INVALID_ARGUMENT, "window must be 0 or an even number of keys in 2..2^25 (got %lld)",
                 (long long)d->window);
-  if (!std::isfinite(d->scale) || !(d->scale > 0.0) || !std::isfinite((float)(d->scale * 1.4426950408889634)) ||
-      !((float)d->scale > 0.f))
-    return fail(MCA_ERR_INVALID_ARGUMENT, "scale must be finite and > 0 in float32 (got %g)", d->scale);
+  // least: the bfloat16 backward pass starts its sums at -lse / scale, |lse| up to 2^22
+  if (!(d->scale >= 0x1p-100) || !std::isfinite((float)(d->scale * 1.4426950408889634)))
+    return fail(MCA_ERR_INVALID_ARGUMENT, "scale must be at least 2^-100 and finite in float32 (got %g)", d->scale);
   if (d->reserved != 0) return fail(MCA_ERR_INVALID_ARGUMENT, "reserved must be 0");
   for (const int32_t* v : {d->q_lens, d->kv_lens, d->q_pos})
     if (reinterpret_cast<uintptr_t>(v) & 3u) return fail(MCA_ERR_INVALID_ARGUMENT, "q_lens, kv_lens and q_pos must be 4-byte aligned");

@@ -5,7 +5,9 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
+import paper_2201_12854_amd as mca  # noqa: E402
 from exact_testutil import Case  # noqa: E402
+from paper_2201_12854_amd import binding  # noqa: E402
 from test_gpu_exact import _check, _make, _run  # noqa: E402
 
 LARGE = [  # B, nq, nk, heads, kv_heads, options; query counts that are no multiple of 32 or 64
@@ -67,3 +69,50 @@ def test_shift_of_ten_thousand(dtype, shape):
     t["table"][:, 0] = -10000.0
     t["table"][:, 1] = 10000.0
     _check(t, kw, bias)
+
+
+SCALED = [
+    (2, 50, 70, 4, 4, {}),
+    (3, 100, 100, 6, 6, dict(causal=True)),  # bfloat16: the gradients in one launch
+    (30, 64, 64, 12, 12, {}),
+    (8, 200, 200, 8, 8, {}),
+    (3, 300, 300, 12, 12, dict(window=40)),
+    (8, 200, 200, 8, 8, dict(buckets=8, max_distance=20)),
+    (2, 3, 2100, 8, 2, dict(causal=True, q_pos=[2097, 5])),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [2.0 ** -100, 2.0 ** -20, 0.01, 1.0, 3.7])
+@pytest.mark.parametrize("shape", SCALED, ids=lambda s: "-".join(map(str, s[:5])) + "".join(f",{k}" for k in s[5]))
+def test_scales(dtype, scale, shape):
+    B, nq, nk, heads, kv, kw = shape
+    print(f"[case] scale {scale} {dtype} {shape}", flush=True)
+    t, kw, bias = _make(dtype, B, nq, nk, heads, kv, **kw)
+    kw["scale"] = scale
+    case = Case(t["Q"], t["K"], t["V"], dY=t["dY"], table=t["table"], **kw, **bias)
+    # Steep rows have P below the smallest normal number 2^-126, which exp2 may return as 0: an error of f = 2^-126
+    # in each P, and so of f max|v| in each of y's nk terms, f max|dy| in each of dv's G nq; of f (|dP| + |D|) in
+    # each dS, |dP| and |D| being at most 64 max|dy| max|v| (y is an average of v), hence in each of the nk terms of dq
+    # and the G nq of dk that times scale max|k| and scale max|q|.
+    f, G = 2.0 ** -126, heads // kv
+    q, k, v, dy = (float(t[n].abs().max()) for n in ("Q", "K", "V", "dY"))
+    lost = f * 128 * dy * v
+    for name, x in dict(Y=nk * f * v, dV=G * nq * f * dy, dQ=scale * nk * lost * k, dK=scale * G * nq * lost * q,
+                        dbias=B * nq * nk * lost).items():
+        if name in case.tol:
+            case.tol[name] = case.tol[name] + x
+    case.check(_run(t, kw, bias))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_small_scales_refused(dtype):
+    """Below 2^-100 (the bfloat16 backward pass starts its sums at -lse / scale)."""
+    t, kw, bias = _make(dtype, 2, 32, 32, 4, 4)
+    f = mca.exact_attention_forward(t["Q"], t["K"], t["V"], **kw)
+    for scale in (2.0 ** -100 * (1 - 2.0 ** -52), 1e-35, 1e-38):
+        for call in (lambda: mca.exact_attention_forward(t["Q"], t["K"], t["V"], **dict(kw, scale=scale)),
+                     lambda: mca.exact_attention_backward(t["dY"], t["Q"], t["K"], t["V"], f.Y, f.lse, **dict(kw, scale=scale))):
+            with pytest.raises(mca.MCAError) as e:
+                call()
+            assert e.value.status == binding.MCA_ERR_INVALID_ARGUMENT
