@@ -253,8 +253,8 @@ mca_status mca_attention_forward_noalloc(const mca_forward_desc* desc, const voi
  *   (the sums of dk and dv run over the H / H_k query heads of the key head too)
  *   dbias_table[c, h] = sum of dS_ij over the pairs of head h in bucket c, all batch rows
  * Logits, softmax statistics and all sums are float32; with bfloat16 inputs P and dS enter
- * their matrix products rounded to bfloat16 (to twice the bits in calls of few keys or
- * queries), and results are rounded once.
+ * their matrix products rounded to bfloat16 (to twice the bits where q_len <= 32 or kv_len <= 32,
+ * P of the forward pass up to kv_len = 128), and results are rounded once.
  * Q, K, V, dY and the bias are expected to be finite (the bias: at most 1e30, or masking); a
  * non-finite value in a row that is read makes the results of its batch row unspecified. The
  * backward pass takes P from lse as it is in float32, to about 2^-17 |lse| of its value: biases of

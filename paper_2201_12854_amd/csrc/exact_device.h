@@ -140,12 +140,17 @@ __device__ __forceinline__ f32x16_t ex_rows_product(const char* tile, const ExRo
   return acc;
 }
 
+// What rounding a and b to the bfloat16 pair w took off, as such a pair.
+__device__ __forceinline__ uint32_t ex_pack_rest(float a, float b, uint32_t w) {
+  return pack_bf16x2(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xffff0000u));
+}
+
 // y[cc] += tile^T x over the tile's 32 rows: rows of y are columns 32 cc .. 32 cc + 31 of the
 // tile. In bf16 x is rounded to bf16 for the product, half a step of the result's own type; FINE: what the
-// rounding took off is multiplied too, in products of its own. (Sums of few terms take that: the roundings of many
-// average out, and bring a result's error in norm from the 1.66e-3 of its own rounding to 2.4e-3, those of
-// a few of nearly equal size, as two keys have them, to 2.9e-3. For all rows it would cost the forward pass
-// 0.3 to 0.7 us of 8, the backward pass 3 to 12%.)
+// rounding took off is multiplied too, in products of its own. Calls of few keys or queries take that: a result's
+// error in norm is then the 1.66e-3 of its own rounding, instead of 2.3e-3 to 2.4e-3. For long rows it would cost 20
+// to 50% (4 x 4096 tokens, 12 heads, forward 204 and 310 us, with the backward pass 924 and 1348; 16 x 512 with a
+// bias 120 and 145; 8 x 1057 under a window 96 and 118).
 template <typename T, bool FINE = false>
 __device__ __forceinline__ void ex_cols_product(f32x16_t (&y)[2], const char* tile, const f32x16_t& x, int lane) {
   const int hf = lane >> 5;
@@ -173,9 +178,7 @@ __device__ __forceinline__ void ex_cols_product(f32x16_t (&y)[2], const char* ti
       }
       if constexpr (FINE) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-          b[w] = pack_bf16x2(x[8 * pp + 2 * w] - __uint_as_float(b[w] << 16),
-                             x[8 * pp + 2 * w + 1] - __uint_as_float(b[w] & 0xffff0000u));
+        for (int w = 0; w < 4; ++w) b[w] = ex_pack_rest(x[8 * pp + 2 * w], x[8 * pp + 2 * w + 1], b[w]);
 #pragma unroll
         for (int cc = 0; cc < 2; ++cc) y[cc] = ex_mfma<T>(t[cc], b, y[cc]);
       }

@@ -218,8 +218,9 @@ __device__ __forceinline__ float ex_row_dot(const ExRow<T>& a, const ExRow<T>& b
   return D;
 }
 
-// FEW of the kernels below: P and dS are multiplied to more than the type's bits (ex_cols_product). For calls
-// of few pairs: up to 32 queries or keys, a tile, where it takes less than 0.5 us.
+// FEW of the kernels below: P and dS are multiplied to more than the type's bits (ex_cols_product). By the lengths
+// alone, so that a row's precision does not depend on how many there are: up to 32 queries or keys, a tile, whose
+// roundings do not average out.
 bool few(const ExactParams& p) { return p.bf16 && std::min(p.nq, p.nk) <= 32; }
 
 // ------------------------------------------------------------------ dQ
@@ -587,7 +588,7 @@ __device__ __forceinline__ ExPair ex_pair(const f32x16_t& s, int j, float fac, f
 
 constexpr float kSmallP = 0x1p-6f;
 
-template <bool BIAS, bool WIN>
+template <bool BIAS, bool WIN, bool FEW>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_dq_tiles(ExactParams p) {
   extern __shared__ __align__(16) char smem[];  // three K tiles, three V tiles, the bias table
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -644,9 +645,9 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
   }
   load(1, 1);
   D += ex_other_half(D);
-  f32x16_t nD;  // where dP's sums start
+  f32x16_t nD;  // where dP's sums start (FEW: at 0, and D is taken off afterwards, which leaves registers for dS)
 #pragma unroll
-  for (int r = 0; r < 16; ++r) nD[r] = -D;
+  for (int r = 0; r < 16; ++r) nD[r] = FEW ? 0.f : -D;
   const float* tl = tb + p.D + 64;
   float rest = 0.f;  // sum of dS
   if constexpr (BIAS) {
@@ -706,8 +707,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
         if (j < 8) e = ex_pair<true>(s, j, fac, add);
         if (j > 0) {
           const int k = j - 1;
-          d[2 * k] *= b4.e0;
-          d[2 * k + 1] *= b4.e1;
+          d[2 * k] = (FEW ? d[2 * k] - D : d[2 * k]) * b4.e0;
+          d[2 * k + 1] = (FEW ? d[2 * k + 1] - D : d[2 * k + 1]) * b4.e1;
           rest += d[2 * k] + d[2 * k + 1];
           pr[2 * k] = b4.e0;
           pr[2 * k + 1] = b4.e1;
@@ -718,6 +719,16 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
         }
       }
       __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (FEW) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        u32x4_t w;
+#pragma unroll
+        for (int l = 0; l < 4; ++l) w[l] = ex_pack_rest(d[8 * k + 2 * l], d[8 * k + 2 * l + 1], ds[k][l]);
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc) dq[cc] = ex_mfma<uint16_t>(ex_read_col(ct, ca, ch, k, cc), w, dq[cc]);
+      }
     }
     if (__builtin_expect(__any(most > kSmallP), 0)) {
 #pragma unroll
@@ -778,7 +789,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
 constexpr int kDkvTilesStage = 2 * kTile64 + 512;  // Q, dY, two planes of 64 statistics
 constexpr int kDkvTilesLds = 3 * kDkvTilesStage;
 
-template <bool BIAS, bool WIN>
+template <bool BIAS, bool WIN, bool FEW>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_dkv_tiles(ExactParams p, int heads_at_once) {
   extern __shared__ __align__(16) char smem[];  // three stages, sums along diagonals, the bias tables of `heads_at_once` heads
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -905,6 +916,7 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
           ex_pin(x);
           pp[k >> 2][k & 3] = w;
           ds[k >> 2][k & 3] = x;
+          if constexpr (FEW) s[2 * k] = b4.e0, s[2 * k + 1] = b4.e1;
         }
       }
       if (BIAS && i == 8) {
@@ -912,9 +924,27 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
         else if (side > 0) far_r += ex_sum16(d);
         else ex_diagonals(diag, d, entry, lane);
       }
-      if (i == 9) start(s, d, ft, fh);
-      if (BIAS && i == 10) peek(in, tn);
+      if (!FEW && i == 9) start(s, d, ft, fh);
+      if (BIAS && !FEW && i == 10) peek(in, tn);
       __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (FEW) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        u32x4_t w, x;
+#pragma unroll
+        for (int l = 0; l < 4; ++l) {
+          w[l] = ex_pack_rest(s[8 * k + 2 * l], s[8 * k + 2 * l + 1], pp[k][l]);
+          x[l] = ex_pack_rest(d[8 * k + 2 * l], d[8 * k + 2 * l + 1], ds[k][l]);
+        }
+#pragma unroll
+        for (int cc = 0; cc < 2; ++cc) {
+          dv[cc] = ex_mfma<uint16_t>(ex_read_col(ct + kTile64, ca, ch, k, cc), w, dv[cc]);
+          dk[cc] = ex_mfma<uint16_t>(ex_read_col(ct, ca, ch, k, cc), x, dk[cc]);
+        }
+      }
+      start(s, d, ft, fh);
+      if constexpr (BIAS) peek(in, tn);
     }
   };
 
@@ -1221,6 +1251,10 @@ bool dkv_in_tiles(const ExactParams& p) {
   return in_tiles(p, (int64_t)((p.nk + 31) / 32) * p.Hk * p.B, p.G * p.nq) || (p.bf16 && (int64_t)p.G * ((p.nq + 31) / 32) > 64);
 }
 
+// k_exact_dkv_tiles with the keys around a window's global one in blocks of their own; not for few queries or keys,
+// whose way is short.
+bool dkv_global_apart(const ExactParams& p) { return p.window && !few(p); }
+
 int dkv_waves(const ExactParams& p) {  // of k_exact_dkv
   const int64_t tiles = (int64_t)p.G * ((p.nq + 31) / 32) / p.kv_splits;
   return p.bf16 && !few(p) && exact_eight_waves((int64_t)((p.nk + 31) / 32) * p.Hk * p.B * p.kv_splits, tiles) ? 8 : 4;
@@ -1252,13 +1286,16 @@ hipError_t launch_dq(const ExactParams& p, hipStream_t s) {
                                                                                                 : launch_dq_of<BIAS, 4, false>(p, s);
   }
   const int64_t blocks = (int64_t)((p.nq + 127) / 128) * p.H * p.B;
-  if (p.window && !p.causal) {
-    const size_t lds = kDqLds<uint16_t, 2, 4> + table_bytes<BIAS>(p);
-    const hipError_t e = exact_set_lds<k_exact_dq_tiles<BIAS, true>>(lds);
+  const size_t table = table_bytes<BIAS>(p);
+  if (few(p)) {
+    hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, false, true>), dim3((unsigned)blocks), dim3(kExThreads), 6 * kTile64 + table, s, p);
+  } else if (p.window && !p.causal) {
+    const size_t lds = kDqLds<uint16_t, 2, 4> + table;
+    const hipError_t e = exact_set_lds<k_exact_dq_tiles<BIAS, true, false>>(lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, true>), dim3((unsigned)(blocks + p.H * p.B)), dim3(kExThreads), lds, s, p);
+    hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, true, false>), dim3((unsigned)(blocks + p.H * p.B)), dim3(kExThreads), lds, s, p);
   } else {
-    hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, false>), dim3((unsigned)blocks), dim3(kExThreads), 6 * kTile64 + table_bytes<BIAS>(p), s, p);
+    hipLaunchKernelGGL((k_exact_dq_tiles<BIAS, false, false>), dim3((unsigned)blocks), dim3(kExThreads), 6 * kTile64 + table, s, p);
   }
   return hipGetLastError();
 }
@@ -1294,9 +1331,10 @@ hipError_t launch_dkv(const ExactParams& p, hipStream_t s) {
     return dkv_waves(p) == 8 ? launch_dkv_of<BIAS, 8, false>(p, s) : launch_dkv_of<BIAS, 4, false>(p, s);
   }
   const int64_t blocks = dkv_blocks(p, 128);
-  if (p.window)
-    return launch_dkv_kernel<k_exact_dkv_tiles<BIAS, true>, BIAS>(p, blocks + (int64_t)p.Hk * p.B, kDkvLds<uint16_t, 2, 4>, s);
-  return launch_dkv_kernel<k_exact_dkv_tiles<BIAS, false>, BIAS>(p, blocks, kDkvTilesLds, s);
+  if (dkv_global_apart(p))
+    return launch_dkv_kernel<k_exact_dkv_tiles<BIAS, true, false>, BIAS>(p, blocks + (int64_t)p.Hk * p.B, kDkvLds<uint16_t, 2, 4>, s);
+  if (few(p)) return launch_dkv_kernel<k_exact_dkv_tiles<BIAS, false, true>, BIAS>(p, blocks, kDkvTilesLds, s);
+  return launch_dkv_kernel<k_exact_dkv_tiles<BIAS, false, false>, BIAS>(p, blocks, kDkvTilesLds, s);
 }
 
 template <bool BIAS>
@@ -1341,7 +1379,7 @@ hipError_t launch_backward(const ExactParams& p, hipStream_t s) {
 // where that saves more than the join takes.
 int exact_kv_splits(const ExactParams& p) {
   const bool big = dkv_in_tiles(p);
-  if ((big && p.window) || exact_backward_small(p)) return 1;
+  if ((big && dkv_global_apart(p)) || exact_backward_small(p)) return 1;
   const int64_t blocks = (int64_t)((p.nk + (big ? 127 : 31)) / (big ? 128 : 32)) * p.Hk * p.B;
   const int64_t tiles = (int64_t)p.G * ((p.nq + (big ? 63 : 31)) / (big ? 64 : 32));
   const int64_t n = std::min((big ? 2 : 1) * device_cus() / blocks, tiles / (big ? 16 : kExWaves));
@@ -1350,7 +1388,7 @@ int exact_kv_splits(const ExactParams& p) {
 
 int64_t exact_bias_parts(const ExactParams& p) {  // a part per wave of k_exact_dkv
   if (!dkv_in_tiles(p)) return (int64_t)p.kv_splits * p.B * ((p.nk + 31) / 32) * dkv_waves(p);
-  return (int64_t)p.B * (p.kv_splits * ((p.nk + 127) / 128) + (p.window ? 1 : 0)) * kExWaves;
+  return (int64_t)p.B * (p.kv_splits * ((p.nk + 127) / 128) + (dkv_global_apart(p) ? 1 : 0)) * kExWaves;
 }
 
 hipError_t launch_exact_backward(const ExactParams& p, hipStream_t s) {

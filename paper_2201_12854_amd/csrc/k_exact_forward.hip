@@ -223,10 +223,10 @@ __global__ __launch_bounds__(kExThreads) void k_exact_join(ExactParams p) {
 }
 
 // ------------------------------------------------------------------ up to 128 queries and keys, bf16
-// For grids that fill the card: a block has a (batch row, head)'s K and V in LDS, a wave 32 of its queries. Bound
-// by memory where there are many (128 x 128 tokens, 12 heads, 19.5 us for 101 MB; in blocks of 128 queries
-// 21.6); a wave for each 32 rows puts more short rows on a CU (300 x 40, 16 heads, 19 and 33 us; 64 x 64 6.5
-// and 8.0; 64 rows of 16 to 128 10.6 and 10.9).
+// For grids that fill the card: a block has a (batch row, head)'s K and V in LDS, a wave for each 32 of its queries,
+// which puts more short rows on a CU than blocks of 128 queries do (300 x 40 tokens, 16 heads, 20 and 35 us; 64 x
+// 64, 12 heads, 7.0 and 8.3; 64 rows of 16 to 128 10.7 and 11.0; 128 x 128, 101 MB, 22.3 and 22.4, of which P's
+// second products are 3).
 __global__ __launch_bounds__(kExThreads) void k_exact_forward_small(ExactParams p) {
   using T = uint16_t;
   extern __shared__ __align__(16) char smem[];  // K, V
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(kExThreads) void k_exact_forward_small(ExactParams 
       for (int r = 0; r < 16; ++r) x[r] *= p.s2;
       if (!ex_whole(p, br.pos + r0, br.pos + last, k0, br.klen)) ex_mask(x, keys, k0 + 4 * hf, k0 > 0);
       ex_softmax_step(s, x);
-      ex_cols_product<T>(s.y, smem + M + 4096 * kt, x, lane);
+      ex_cols_product<T, true>(s.y, smem + M + 4096 * kt, x, lane);
     }
   }
   s.l += ex_other_half(s.l);
@@ -286,7 +286,9 @@ __global__ __launch_bounds__(kExThreads) void k_exact_forward_small(ExactParams 
 // correction of what has been summed, and keeps its relative precision, in bf16 too, up to the
 // type's range. A row whose sum passes 2^64 (logits 44 above M), or whose first keys the bias all
 // masked and whose sum is below 2^-20, has its block take the pass again with a running maximum.
-template <bool BIAS, int MT, bool WIN>
+//
+// FEW: as of k_exact_rows. What the rounding of P took off goes through an MFMA of its own, behind that of P V.
+template <bool BIAS, int MT, bool WIN, bool FEW>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 3 : 2))) void k_exact_tiles(ExactParams p) {
   constexpr int QB = 128 * MT;
   extern __shared__ __align__(16) char smem[];  // three K tiles, three V tiles, the bias table
@@ -349,13 +351,17 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
   const ExCols64<true> va = ex_cols64<true>(lane);
   const f32x16_t zero = ex_zero16();
   f32x16_t y[MT][2], s0[MT], s1[MT];
-  u32x4_t pa[MT][2], pb[MT][2];  // P of a half tile, 16 keys each
+  struct P16 {
+    u32x4_t v[2], rest[FEW ? 2 : 1];
+  };
+  P16 pa[MT], pb[MT];  // P of a half tile, 16 keys each
   u32x4_t kf[4], vf[2][2];
   float l[MT], nm[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     y[m][0] = y[m][1] = zero;
-    pb[m][0] = pb[m][1] = u32x4_t{0u, 0u, 0u, 0u};  // the first P V multiplies zeros
+    pb[m].v[0] = pb[m].v[1] = u32x4_t{0u, 0u, 0u, 0u};  // the first P V multiplies zeros
+    if constexpr (FEW) pb[m].rest[0] = pb[m].rest[1] = pb[m].v[0];
     l[m] = 0.f;
   }
   vf[0][0] = vf[0][1] = vf[1][0] = vf[1][1] = u32x4_t{0u, 0u, 0u, 0u};
@@ -409,8 +415,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
   };
   // Half tile h: P of cur into po, S of half tile h + 1 into nxt, P V of half tile h - 1 (pi, vf); K half
   // tile h + 2 and V half tile h are `half` of the tiles at kt and vt.
-  auto step = [&](f32x16_t (&cur)[MT], f32x16_t (&nxt)[MT], const u32x4_t (&pi)[MT][2], u32x4_t (&po)[MT][2],
-                  const char* kt, const char* vt, int half) __attribute__((always_inline)) {
+  auto step = [&](f32x16_t (&cur)[MT], f32x16_t (&nxt)[MT], const P16 (&pi)[MT], P16 (&po)[MT], const char* kt, const char* vt,
+                  int half) __attribute__((always_inline)) {
     float e0 = 0.f, e1 = 0.f;
 #pragma unroll
     for (int j = 0; j < 8 * MT; ++j) {
@@ -420,7 +426,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
         __builtin_amdgcn_sched_barrier(0);  // the reload takes the registers the MFMA has read
         if (m == MT - 1) kf[i] = ex_read_row(kt, ka, half, i);
       } else {
-        y[m][cc] = ex_mfma<uint16_t>(vf[pp][cc], pi[m][pp], y[m][cc]);
+        y[m][cc] = ex_mfma<uint16_t>(vf[pp][cc], pi[m].v[pp], y[m][cc]);
+        if constexpr (FEW) y[m][cc] = ex_mfma<uint16_t>(vf[pp][cc], pi[m].rest[pp], y[m][cc]);
         __builtin_amdgcn_sched_barrier(0);
         if (m == MT - 1) vf[pp][cc] = ex_read_col(vt, va, half, pp, cc);
       }
@@ -433,7 +440,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
         l[o] += e1;
         uint32_t w = pack_bf16x2(e0, e1);
         ex_pin(w);
-        po[o][((j - 1) >> 2) & 1][(j - 1) & 3] = w;
+        po[o].v[((j - 1) >> 2) & 1][(j - 1) & 3] = w;
+        if constexpr (FEW) po[o].rest[((j - 1) >> 2) & 1][(j - 1) & 3] = ex_pack_rest(e0, e1, w);
       }
       e0 = ex_exp2(x0);
       e1 = ex_exp2(x1);
@@ -443,7 +451,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
     }
     l[MT - 1] += e0;
     l[MT - 1] += e1;
-    po[MT - 1][1][3] = pack_bf16x2(e0, e1);
+    po[MT - 1].v[1][3] = pack_bf16x2(e0, e1);
+    if constexpr (FEW) po[MT - 1].rest[1][3] = ex_pack_rest(e0, e1, po[MT - 1].v[1][3]);
   };
 
   if constexpr (BIAS) __syncthreads();
@@ -486,7 +495,10 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int m = 0; m < MT; ++m) y[m][i & 1] = ex_mfma<uint16_t>(vf[i >> 1][i & 1], pb[m][i >> 1], y[m][i & 1]);
+    for (int m = 0; m < MT; ++m) {
+      y[m][i & 1] = ex_mfma<uint16_t>(vf[i >> 1][i & 1], pb[m].v[i >> 1], y[m][i & 1]);
+      if constexpr (FEW) y[m][i & 1] = ex_mfma<uint16_t>(vf[i >> 1][i & 1], pb[m].rest[i >> 1], y[m][i & 1]);
+    }
   wait_vmcnt<0>();  // no load is under way into what is written next
   bool again = false;
 #pragma unroll
@@ -538,12 +550,18 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
           ex_softmax_step(s, x);
 #pragma unroll
           for (int pp = 0; pp < 2; ++pp) {
-            u32x4_t x8;
+            u32x4_t x8, rest;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) x8[w] = pack_bf16x2(x[8 * pp + 2 * w], x[8 * pp + 2 * w + 1]);
+            for (int w = 0; w < 4; ++w) {
+              x8[w] = pack_bf16x2(x[8 * pp + 2 * w], x[8 * pp + 2 * w + 1]);
+              if constexpr (FEW) rest[w] = ex_pack_rest(x[8 * pp + 2 * w], x[8 * pp + 2 * w + 1], x8[w]);
+            }
 #pragma unroll
-            for (int cc = 0; cc < 2; ++cc)
-              s.y[cc] = ex_mfma<uint16_t>(ex_read_col(smem + 3 * kTile64, vc, half, pp, cc), x8, s.y[cc]);
+            for (int cc = 0; cc < 2; ++cc) {
+              const u32x4_t v = ex_read_col(smem + 3 * kTile64, vc, half, pp, cc);
+              s.y[cc] = ex_mfma<uint16_t>(v, x8, s.y[cc]);
+              if constexpr (FEW) s.y[cc] = ex_mfma<uint16_t>(v, rest, s.y[cc]);
+            }
           }
         }
         __syncthreads();
@@ -558,17 +576,17 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(MT =
   for (int m = 0; m < MT; ++m) store(m, nm[m], l[m], y[m]);
 }
 
-template <bool BIAS, int MT, bool WIN>
+template <bool BIAS, int MT, bool WIN, bool FEW = false>
 hipError_t launch_tiles(const ExactParams& p, hipStream_t s) {
   const size_t table = BIAS ? (size_t)exact_bias_entries(p.D) * 4 : 0;
   const size_t lds = table + (WIN ? (size_t)kRowLds<uint16_t, 2, 4> : 6 * kTile64);
   const int64_t blocks = ((int64_t)((p.nq + 128 * MT - 1) / (128 * MT)) + WIN) * p.H * p.B;
   if constexpr (WIN) {
-    const hipError_t e = exact_set_lds<k_exact_tiles<BIAS, MT, WIN>, 512>(lds);
+    const hipError_t e = exact_set_lds<k_exact_tiles<BIAS, MT, WIN, FEW>, 512>(lds);
     if (e != hipSuccess) return e;
   }
   static_assert(6 * kTile64 + (2 * kMaxBiasDistance + 129) * 4 <= 65536 - 512, "LDS that needs no leave");
-  hipLaunchKernelGGL((k_exact_tiles<BIAS, MT, WIN>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
+  hipLaunchKernelGGL((k_exact_tiles<BIAS, MT, WIN, FEW>), dim3((unsigned)blocks), dim3(kExThreads), lds, s, p);
   return hipGetLastError();
 }
 
@@ -584,9 +602,11 @@ hipError_t launch_rows_of(const ExactParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-// FEW: P is multiplied to more than the type's bits (ex_cols_product). Up to these many keys, a tile to each
-// wave.
-constexpr int kFewKeys = 128;
+// FEW of the kernels above: P is multiplied to more than the type's bits (ex_cols_product). By the lengths alone, so
+// that a row's precision does not depend on how many there are: up to 128 keys, a tile to each wave of a block, or
+// up to 32 queries (32 x 1 token, 16 heads on 4, up to 16384 keys, 73.2 and 73.6 us; 1 x 1, 701 keys, 7.5 and 7.9; 64
+// rows of 16 to 128 tokens, 12 heads, 11.5 and 12.5).
+bool few(const ExactParams& p) { return p.bf16 && (p.nk <= 128 || p.nq <= 32); }
 
 // bf16: two tiles, 64 KB of LDS for a block, two of them to a CU. float32, whose tiles are twice as large: two
 // where every block has a CU of its own, else one and two blocks to a CU, which cover each other's loads
@@ -597,8 +617,9 @@ hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
   if constexpr (ExFmt<T>::ES == 4) {
     if (blocks > device_cus()) return launch_rows_of<T, BIAS, 1, 4>(p, s);
   } else {
-    if (p.nk <= kFewKeys) return launch_rows_of<T, BIAS, 2, 4, true>(p, s);
-    if (exact_eight_waves(blocks, ((p.nk + 31) / 32) / p.splits)) return launch_rows_of<T, BIAS, 2, 8>(p, s);
+    const bool eight = exact_eight_waves(blocks, ((p.nk + 31) / 32) / p.splits);
+    if (few(p)) return eight ? launch_rows_of<T, BIAS, 2, 8, true>(p, s) : launch_rows_of<T, BIAS, 2, 4, true>(p, s);
+    if (eight) return launch_rows_of<T, BIAS, 2, 8>(p, s);
   }
   return launch_rows_of<T, BIAS, 2, 4>(p, s);
 }
@@ -612,9 +633,10 @@ int exact_group(const ExactParams& p) {
 }
 
 // bf16 in blocks of 128 queries or more, or of a whole short row: where the blocks of 32 rows are more than the CUs
-// (forward, 12 heads: 8 x 128 tokens, 384 blocks of 32, 6.9 against 5.7 us; 1 x 1024 23.8 and 16.6; 2 x 256, 192
-// blocks, 6.1 and 7.8; 1 x 512 7.5 and 10.5). Rows of a single block of 32 over many keys
-// stay: its four waves share the keys, of which a wave of the other kernel reads all.
+// (forward, 12 heads: 8 x 128 tokens, 384 blocks of 32, 7.1 against 6.8 us; 8 x 160 7.4 and 7.1; 3 x 300 8.5 and 8.3;
+// 2 x 256, 192 blocks, 6.9 and 7.5; 1 x 512 7.4 and 10.3). Long rows that are not many more blocks would still be
+// faster in blocks of 32 (1 x 1024 13.0 and 16.6; 2 x 2048, 4 heads, 21.9 and 28.3). Rows of a single block of 32 over
+// many keys stay: its four waves share the keys, of which a wave of the other kernel reads all.
 static bool forward_in_tiles(const ExactParams& p) {
   return p.bf16 && exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B > device_cus() &&
          (p.nq * p.Gp > 32 || p.nk <= 512);
@@ -633,9 +655,9 @@ static bool forward_wide(const ExactParams& p) {
 // Blocks that share a row's keys. Enough to give every CU one, of three tiles to a wave at least (float32,
 // whose tiles take four times as long: less than one); or, where the keys are so long that sixteen tiles
 // stay to a wave (four), up to four to a CU, which even out rows of different lengths. Not for less than
-// the join takes. A token, 12 heads, bf16: 1500 keys 12.3 us in one part, 9.7 in 4, 10.2 in 8; 4000 keys
-// 25.5, 13.0, 11.5; 16000 keys 111, 20.5 in 16; 701 keys 8.3, 9.0 in 4. 32 tokens, 16 heads on 4, 2048 to
-// 16384 keys: 86.5 us in 2 parts, 66.9 in 8, 80.3 in 32.
+// the join takes. A token, 12 heads, bf16: 1500 keys 10.6 us in one part, 10.4 in 4, 10.0 in 8; 4000 keys
+// 20.0, 12.2, 10.3; 16000 keys 72.2, 15.9 in 16; 701 keys 7.7, 10.0 in 4. 32 rows of one token, 16
+// heads on 4, 2048 to 16384 keys: 65.8 us in 2 parts, 63.6 in 8, 71.8 in 32.
 int exact_splits(const ExactParams& p) {
   if (forward_in_tiles(p)) return 1;
   const int64_t rows = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B, tiles = (p.nk + 31) / 32;
@@ -646,8 +668,8 @@ int exact_splits(const ExactParams& p) {
 }
 
 // Eight waves to a block instead of four, bf16: where every block has a CU of its own and more than two tiles to
-// a wave (a token, 12 heads: 1024 keys 9.7 us with four waves, 8.3 with eight, 701 keys 8.5 and 7.6, 300 keys,
-// 10 tiles, 6.7 and 6.6; 2 x 1024 tokens, 4 heads, forward 10.5 and 9.2, backward 27.8 and 24.7; backward
+// a wave (a token, 12 heads: 1024 keys 10.0 us with four waves, 8.6 with eight, 701 keys 8.7 and 7.8, 300 keys,
+// 10 tiles, 7.0 and 7.1; 2 x 1024 tokens, 4 heads, forward 10.8 and 9.1, backward 27.8 and 24.7; backward
 // 2 x 256, 8 tiles, 15.0 and 16.6). Not float32, which its matrix instructions bound: 1 x 512 tokens, forward
 // and backward, 74 and 72; 4 x 201, 8 heads on 2, with a bias, 59 and 61.
 bool exact_eight_waves(int64_t blocks, int64_t tiles) { return tiles > 8 && blocks <= device_cus(); }
@@ -659,6 +681,7 @@ hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s) {
     return hipGetLastError();
   }
   if (forward_in_tiles(p)) {
+    if (few(p)) return p.table ? launch_tiles<true, 1, false, true>(p, s) : launch_tiles<false, 1, false, true>(p, s);
     if (p.window && !p.causal) return p.table ? launch_tiles<true, 1, true>(p, s) : launch_tiles<false, 1, true>(p, s);
     if (p.table) return launch_tiles<true, 1, false>(p, s);
     return forward_wide(p) ? launch_tiles<false, 2, false>(p, s) : launch_tiles<false, 1, false>(p, s);
