@@ -1,5 +1,5 @@
 """The limits of test_gpu_exact_precision on the CPU: the arithmetic of the bfloat16 kernels, rounded where they
-round and in float64 elsewhere, stays below them, and would not without the second products."""
+round and in float64 elsewhere, stays below them, and would not without the exact D or without the second products."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -44,6 +44,14 @@ def test_one_rounding(width):
     x = width * torch.randn(100000, generator=torch.Generator().manual_seed(1), dtype=torch.float64)
     for x in (x, x * x, x.sign() * x.abs().exp(), 2 * width * torch.rand(100000, generator=torch.Generator().manual_seed(2), dtype=torch.float64)):
         assert float((_bf16(x) - x).norm() / x.norm()) <= STEP
+
+
+@pytest.mark.parametrize("nq,nk", [(300, 300), (128, 128)])
+def test_exact_d(nq, nk):
+    limit = 2 ** 0.5 * STEP
+    assert all(v <= limit for v in _attention(nq, nk, 6, 4.0, _bf16, True).values())
+    without = _attention(nq, nk, 6, 4.0, _bf16, False)
+    assert min(without["dQ"], without["dK"]) > 1.3 * limit
 
 
 @pytest.mark.parametrize("nq,nk", [(300, 2), (2, 300), (300, 7), (40, 2)])

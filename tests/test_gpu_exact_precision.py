@@ -80,3 +80,22 @@ def test_forward_of_128_keys(shape, q_scale):
     off = _errors(*_make("bf16", B, nq, nk, heads, kv, q_scale=q_scale, **kw), train=False)
     print(off, flush=True)
     assert off["Y"] <= STEP, off
+
+
+@pytest.mark.parametrize("shape", [
+    (2, 300, 300, 3, 3, {}),  # blocks of 32 rows
+    (2, 300, 300, 4, 1, {}),
+    (8, 300, 300, 12, 12, {}),  # of 128
+    (8, 300, 300, 12, 12, dict(causal=True)),
+    (4, 700, 700, 12, 12, dict(window=256)),
+    (8, 300, 300, 12, 12, dict(buckets=32)),
+    (8, 128, 128, 12, 12, {}),  # one launch
+    (3, 100, 100, 4, 4, {}),
+], ids=lambda s: "-".join(map(str, s[:5])) + "".join(f",{k}" for k in s[5]))
+def test_sharp_rows(shape):
+    """Logits of standard deviation 4: with the D of the rounded Y the gradients of Q and K would be 4e-3 off."""
+    B, nq, nk, heads, kv, kw = shape
+    print(f"[case] sharp {shape}", flush=True)
+    off = _errors(*_make("bf16", B, nq, nk, heads, kv, q_scale=4.0, **kw))
+    print(off, flush=True)
+    assert all(v <= 2 ** 0.5 * STEP for v in off.values()), off
