@@ -92,6 +92,12 @@ int exact_splits(const ExactParams& p);
 int exact_kv_splits(const ExactParams& p);
 int64_t exact_bias_parts(const ExactParams& p);
 int exact_group(const ExactParams& p);  // Gp
+// Kernels that a call's sizes choose: in blocks of 32 rows (all float32 calls), of a whole short row, of 128 rows, of
+// 256. The backward pass for dQ and for dK and dV.
+enum class ExactKernel { kRows32, kShort, kRows128, kRows256 };
+ExactKernel exact_forward_kernel(const ExactParams& p);
+ExactKernel exact_dq_kernel(const ExactParams& p);
+ExactKernel exact_dkv_kernel(const ExactParams& p);
 hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s);
 hipError_t launch_exact_backward(const ExactParams& p, hipStream_t s);
 

@@ -1391,6 +1391,13 @@ int64_t exact_bias_parts(const ExactParams& p) {  // a part per wave of k_exact_
   return (int64_t)p.B * (p.kv_splits * ((p.nk + 127) / 128) + (dkv_global_apart(p) ? 1 : 0)) * kExWaves;
 }
 
+ExactKernel exact_dq_kernel(const ExactParams& p) {
+  return exact_backward_small(p) ? ExactKernel::kShort : dq_in_tiles(p) ? ExactKernel::kRows128 : ExactKernel::kRows32;
+}
+ExactKernel exact_dkv_kernel(const ExactParams& p) {
+  return exact_backward_small(p) ? ExactKernel::kShort : dkv_in_tiles(p) ? ExactKernel::kRows128 : ExactKernel::kRows32;
+}
+
 hipError_t launch_exact_backward(const ExactParams& p, hipStream_t s) {
   if (p.bf16) return p.table ? launch_backward<uint16_t, true>(p, s) : launch_backward<uint16_t, false>(p, s);
   return p.table ? launch_backward<float, true>(p, s) : launch_backward<float, false>(p, s);

@@ -674,17 +674,26 @@ int exact_splits(const ExactParams& p) {
 // and backward, 74 and 72; 4 x 201, 8 heads on 2, with a bias, 59 and 61.
 bool exact_eight_waves(int64_t blocks, int64_t tiles) { return tiles > 8 && blocks <= device_cus(); }
 
+ExactKernel exact_forward_kernel(const ExactParams& p) {
+  if (!forward_in_tiles(p)) return ExactKernel::kRows32;
+  if (exact_small(p)) return ExactKernel::kShort;
+  return !few(p) && forward_wide(p) ? ExactKernel::kRows256 : ExactKernel::kRows128;
+}
+
 hipError_t launch_exact_forward(const ExactParams& p, hipStream_t s) {
-  if (exact_small(p) && forward_in_tiles(p)) {
-    const int rows = exact_small_rows(p);
-    hipLaunchKernelGGL(k_exact_forward_small, dim3((unsigned)(p.H * p.B)), dim3(2 * rows), rows * 256, s, p);
-    return hipGetLastError();
-  }
-  if (forward_in_tiles(p)) {
-    if (few(p)) return p.table ? launch_tiles<true, 1, false, true>(p, s) : launch_tiles<false, 1, false, true>(p, s);
-    if (p.window && !p.causal) return p.table ? launch_tiles<true, 1, true>(p, s) : launch_tiles<false, 1, true>(p, s);
-    if (p.table) return launch_tiles<true, 1, false>(p, s);
-    return forward_wide(p) ? launch_tiles<false, 2, false>(p, s) : launch_tiles<false, 1, false>(p, s);
+  const int rows = exact_small_rows(p);
+  switch (exact_forward_kernel(p)) {
+    case ExactKernel::kShort:
+      hipLaunchKernelGGL(k_exact_forward_small, dim3((unsigned)(p.H * p.B)), dim3(2 * rows), rows * 256, s, p);
+      return hipGetLastError();
+    case ExactKernel::kRows256:
+      return launch_tiles<false, 2, false>(p, s);
+    case ExactKernel::kRows128:
+      if (few(p)) return p.table ? launch_tiles<true, 1, false, true>(p, s) : launch_tiles<false, 1, false, true>(p, s);
+      if (p.window && !p.causal) return p.table ? launch_tiles<true, 1, true>(p, s) : launch_tiles<false, 1, true>(p, s);
+      return p.table ? launch_tiles<true, 1, false>(p, s) : launch_tiles<false, 1, false>(p, s);
+    default:
+      break;
   }
   if (p.bf16) return p.table ? launch_rows<uint16_t, true>(p, s) : launch_rows<uint16_t, false>(p, s);
   return p.table ? launch_rows<float, true>(p, s) : launch_rows<float, false>(p, s);
