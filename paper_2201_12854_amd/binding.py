@@ -397,6 +397,12 @@ def _int32(name, v) -> int:
     return int(v)
 
 
+def _int64(name, v) -> int:
+    if not -2**63 <= int(v) < 2**63:
+        raise ValueError(f"{name} must be a 64-bit integer (got {v})")
+    return int(v)
+
+
 def relative_buckets(buckets: int, max_distance: int = 128, bidirectional: bool = True) -> list:
     """The bucket of every relative position -max_distance .. max_distance (further ones share the
     end's), as a list of 2 max_distance + 1 integers."""
@@ -451,7 +457,7 @@ class _ExactCall:
             if t is not None and (t.dtype != torch.int32 or t.shape != (B,) or t.device != dev or not t.is_contiguous()):
                 raise ValueError(f"{name} must be contiguous int32 [{B}] on {dev}")
             lens.append(None if t is None else t.data_ptr())
-        d = self.desc = ExactDesc(B, nq, nk, heads, kv_heads, 64, _dtype_code(Q), int(bool(causal)), int(window),
+        d = self.desc = ExactDesc(B, nq, nk, heads, kv_heads, 64, _dtype_code(Q), int(bool(causal)), _int64("window", window),
                                   0.125 if scale is None else float(scale), *lens)
         self.table = None
         if bias is not None:

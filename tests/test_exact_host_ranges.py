@@ -17,3 +17,11 @@ def test_small_scales_refused(dtype, scale):
     assert _forward(_desc(dtype=dtype, scale=scale)) == binding.MCA_ERR_INVALID_ARGUMENT
     assert _backward(_desc(dtype=dtype, scale=scale)) == binding.MCA_ERR_INVALID_ARGUMENT
     assert "2^-100" in mca.load_library().mca_last_error().decode()
+
+
+def test_wide_window_refused():
+    """Not taken modulo 2^64, where 2^64 + 2 would be a window of 2 and 2^64 none."""
+    for window in (2**64, 2**64 + 2, 2**63, -2**63 - 2):
+        with pytest.raises(ValueError):
+            binding._int64("window", window)
+    assert binding._int64("window", 256) == 256 and binding._int64("window", -2**63) == -2**63

@@ -116,3 +116,14 @@ def test_small_scales_refused(dtype):
             with pytest.raises(mca.MCAError) as e:
                 call()
             assert e.value.status == binding.MCA_ERR_INVALID_ARGUMENT
+
+
+def test_wide_window_refused():
+    t, kw, bias = _make("bf16", 2, 32, 32, 4, 4)
+    for window in (2**64, 2**64 + 2, -2**64 + 2):
+        with pytest.raises(ValueError):
+            mca.exact_attention_forward(t["Q"], t["K"], t["V"], **dict(kw, window=window))
+        with pytest.raises(ValueError):
+            mca.ExactPlan(t["Q"], t["K"], t["V"], **dict(kw, window=window))
+    with pytest.raises(mca.MCAError):
+        mca.exact_attention_forward(t["Q"], t["K"], t["V"], **dict(kw, window=2**63 - 1))
