@@ -1,5 +1,5 @@
 // Prints which kernels calls of exact attention take, for sizes on stdin: bf16 batch q_len kv_len heads kv_heads causal
-// window max_distance (0: no bias). Without a device the rules go by 256 CUs, an MI355X's.
+// window max_distance (0: no bias); then how many parts a bias gradient is joined from. Without a device the rules go by 256 CUs, an MI355X's.
 #include <cstdio>
 #include <cstring>
 
@@ -15,8 +15,9 @@ int main() {
     p.causal = causal, p.window = window > 0, p.half = window / 2, p.D = D;
     p.table = D ? &p : nullptr;  // not read
     p.Gp = mca::exact_group(p);
-    std::printf("%s %s %s\n", names[(int)mca::exact_forward_kernel(p)], names[(int)mca::exact_dq_kernel(p)],
-                names[(int)mca::exact_dkv_kernel(p)]);
+    p.kv_splits = mca::exact_kv_splits(p);
+    std::printf("%s %s %s %lld\n", names[(int)mca::exact_forward_kernel(p)], names[(int)mca::exact_dq_kernel(p)],
+                names[(int)mca::exact_dkv_kernel(p)], (long long)mca::exact_bias_parts(p));
   }
   return 0;
 }
