@@ -524,8 +524,10 @@ def exact_attention_forward(Q, K, V, *, heads: int, kv_heads: Optional[int] = No
     query: for a few new tokens behind a cached prefix, kv_lens - n_q. ``causal``: keys up to the
     query's position. ``window``: 0, or an even local window with a global first token. ``bias``: a
     RelativeBias. ``out`` may pass preallocated (Y, lse).
+    ``workspace``: a tensor to work in; one that is too small, or None, is replaced by a new one.
     Returns Y [B, n_q, heads*64] of Q's dtype and lse [B, heads, n_q] float32 (-inf where a query
-    attends no key; its Y is 0).
+    attends no key; its Y is 0). torch's automatic differentiation does not see the call, whatever the
+    inputs ask for: gradients come from ``exact_attention_backward``.
     """
     lib = load_library()
     call = _ExactCall(Q, K, V, heads, kv_heads, scale, q_lens, kv_lens, q_pos, causal, window, bias)
