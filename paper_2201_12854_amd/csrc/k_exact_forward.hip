@@ -608,20 +608,20 @@ hipError_t launch_rows_of(const ExactParams& p, hipStream_t s) {
 // rows of 16 to 128 tokens, 12 heads, 11.5 and 12.5).
 bool few(const ExactParams& p) { return p.bf16 && (p.nk <= 128 || p.nq <= 32); }
 
-// bf16: two tiles, 64 KB of LDS for a block, two of them to a CU. float32, whose tiles are twice as large: two
-// where every block has a CU of its own, else one and two blocks to a CU, which cover each other's loads
-// (forward, 12 heads: 2 x 333 tokens, one block to a CU, 14.6 against 15.5 us; 32 x 128, six, 48 against 36).
+// bf16: two tiles, 64 KB of LDS for a block, two of them to a CU. float32, whose tiles are twice as large: one, and two
+// blocks to a CU, which cover each other's loads (forward, 12 heads, two tiles against one: 32 x 128 tokens 50.0 and
+// 34.2 us; 2 x 320, where every block has a CU of its own, 14.7 and 14.1; 1 x 128 7.9 and 7.2; 32 x 1, 16 heads on 4,
+// 16384 keys, 240 and 197).
 template <typename T, bool BIAS>
 hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
   const int64_t blocks = exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B * p.splits;
   if constexpr (ExFmt<T>::ES == 4) {
-    if (blocks > device_cus()) return launch_rows_of<T, BIAS, 1, 4>(p, s);
+    return launch_rows_of<T, BIAS, 1, 4>(p, s);
   } else {
     const bool eight = exact_eight_waves(blocks, ((p.nk + 31) / 32) / p.splits);
     if (few(p)) return eight ? launch_rows_of<T, BIAS, 2, 8, true>(p, s) : launch_rows_of<T, BIAS, 2, 4, true>(p, s);
-    if (eight) return launch_rows_of<T, BIAS, 2, 8>(p, s);
+    return eight ? launch_rows_of<T, BIAS, 2, 8>(p, s) : launch_rows_of<T, BIAS, 2, 4>(p, s);
   }
-  return launch_rows_of<T, BIAS, 2, 4>(p, s);
 }
 
 }  // namespace
@@ -629,7 +629,7 @@ hipError_t launch_rows(const ExactParams& p, hipStream_t s) {
 // Heads side by side in the kernels of 32 rows: a key head's whole group, unless its bias tables do not
 // fit beside the tiles.
 int exact_group(const ExactParams& p) {
-  return !p.table || (int64_t)p.G * exact_bias_entries(p.D) * 4 <= (int64_t)kMaxLds - kRowLds<float, 2, 4> ? p.G : 1;
+  return !p.table || (int64_t)p.G * exact_bias_entries(p.D) * 4 <= (int64_t)kMaxLds - kRowLds<uint16_t, 2, 8> ? p.G : 1;
 }
 
 // bf16 in blocks of 128 queries or more, or of a whole short row: where the blocks of 32 rows are more than the CUs
