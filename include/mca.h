@@ -303,8 +303,8 @@ typedef struct mca_rows {
 
 /*
  * Bytes of device workspace of mca_exact_attention_forward (backward = 0) or
- * mca_exact_attention_backward (backward = 1) for `desc` (host only); may be 0. Errors: as
- * their checks of desc.
+ * mca_exact_attention_backward (backward = 1) for `desc` on the current device (host only); may
+ * be 0. Errors: as their checks of desc.
  */
 mca_status mca_exact_workspace_size(const mca_exact_desc* desc, int backward, size_t* bytes);
 

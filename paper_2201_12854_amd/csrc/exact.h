@@ -62,8 +62,8 @@ constexpr int kSmallRows = 128;
 inline bool exact_small(const ExactParams& p) { return p.bf16 && !p.table && p.nq <= kSmallRows && p.nk <= kSmallRows; }
 inline bool exact_backward_small(const ExactParams& p) { return exact_small(p) && p.G == 1; }
 // Rows that such a block has room for, 32 for each of its waves: with fewer waves more blocks are on a CU
-// (backward pass, against four always: 128 x 32 tokens, 12 heads, 13.0 and 19.9 us, 64 x 64 15.0 and 17.7, 300 x
-// 40, 16 heads, 49 and 73).
+// (backward pass, against four always: 128 x 32 tokens, 12 heads, 12.4 and 19.9 us, 64 x 64 14.2 and 17.7, 300 x
+// 40, 16 heads, 46 and 73).
 __host__ __device__ inline int exact_small_rows(const ExactParams& p) { return ((p.nq > p.nk ? p.nq : p.nk) + 31) / 32 * 32; }
 
 constexpr size_t kMaxLds = 163840;  // of a block: a CU's

@@ -1074,8 +1074,8 @@ __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2)))
 // ------------------------------------------------------------------ up to 128 queries and keys, bf16
 // One launch for all three gradients: a block has a (batch row, head)'s Q, K, V and dY in LDS, its four waves
 // take 32 queries each for D and dQ, and then 32 keys each for dK and dV. What two launches cost at this size is
-// mostly their starts and loads (backward pass, 12 heads, two launches against one: 1 x 32 tokens 11.4 and 6.1
-// us; 1 x 128 11.8 and 10.4; 32 x 128 24.7 and 18.7; 128 x 128 69 and 51).
+// mostly their starts and loads (backward pass, 12 heads, two launches against one: 1 x 32 tokens 13.1 and 7.4
+// us; 1 x 128 13.3 and 10.4; 32 x 128 23.6 and 17.9; 128 x 128 69 and 48).
 template <bool FEW>
 __global__ __launch_bounds__(kExThreads) __attribute__((amdgpu_waves_per_eu(2))) void k_exact_backward_small(ExactParams p) {
   using T = uint16_t;
@@ -1239,14 +1239,15 @@ __global__ __launch_bounds__(kExThreads) void k_exact_join_grads(ExactParams p, 
 
 // bf16 in blocks of 128 rows where the blocks of 32 are more than the CUs, or, in a long loop, which is all a
 // block of 128 has on a CU then, twice as many (backward pass, 12 heads: 4 x 256 tokens, 384 blocks of 32,
-// 22.4 against 18.6 us; 2 x 512 26.1 and 31.9; 1 x 1024 34.4 and 44.1; 2 x 256, 192 blocks, 13.5 and 18.2).
+// 22.3 against 20.0 us; 2 x 512 26.1 and 28.8; 1 x 1024 34.5 and 45.5; 2 x 256, 192 blocks, 15.1 and 19.8).
 bool in_tiles(const ExactParams& p, int64_t blocks, int loop) {
   return p.bf16 && blocks > (loop > 384 ? 2 : 1) * (int64_t)device_cus();
 }
 bool dq_in_tiles(const ExactParams& p) { return in_tiles(p, exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B, p.nk); }
 // And where a block of 32 keys would have a long way over the queries of its heads (64 tiles), which blocks of
-// 128 keys then share (exact_kv_splits): 2 x 1024 tokens, 16 heads on 2, 66 against 61 us; 1 x 8192, 1 head,
-// 130 and 107; 1 x 2048, 4 heads, 41 against 47.
+// 128 keys then share (exact_kv_splits): backward pass, 1 x 16384 tokens, 1 head, 335 against 295 us; 1 x 4096, 8
+// heads on 2, 158 and 149; 1 x 8192, 1 head, and 2 x 1024, 16 on 2, as long either way; 1 x 2048, 4 heads, 64 tiles,
+// 35 and 46. (Where the blocks of 32 leave CUs without one it takes longer: 1 x 4096, 2 heads on 1, 58 and 64.)
 bool dkv_in_tiles(const ExactParams& p) {
   return in_tiles(p, (int64_t)((p.nk + 31) / 32) * p.Hk * p.B, p.G * p.nq) || (p.bf16 && (int64_t)p.G * ((p.nq + 31) / 32) > 64);
 }

@@ -635,7 +635,7 @@ int exact_group(const ExactParams& p) {
 // bf16 in blocks of 128 queries or more, or of a whole short row: where the blocks of 32 rows are more than the CUs
 // (forward, 12 heads: 8 x 128 tokens, 384 blocks of 32, 7.1 against 6.8 us; 8 x 160 7.4 and 7.1; 3 x 300 8.5 and 8.3;
 // 2 x 256, 192 blocks, 6.9 and 7.5; 1 x 512 7.4 and 10.3). Long rows that are not many more blocks would still be
-// faster in blocks of 32 (1 x 1024 13.0 and 16.6; 2 x 2048, 4 heads, 21.9 and 28.3). Rows of a single block of 32 over
+// faster in blocks of 32 (1 x 1024 13.6 and 16.4; 1 x 2048, 8 heads, 22.3 and 28.4). Rows of a single block of 32 over
 // many keys stay: its four waves share the keys, of which a wave of the other kernel reads all.
 static bool forward_in_tiles(const ExactParams& p) {
   return p.bf16 && exact_row_tiles(p.nq, p.Gp) * (p.H / p.Gp) * p.B > device_cus() &&
@@ -643,8 +643,8 @@ static bool forward_in_tiles(const ExactParams& p) {
 }
 // 256 queries per block instead of 128 halve the LDS reads and the loads per score, and take about 1.75
 // times as long: by what the CU with the most blocks has to do (4 x 4096 tokens, 12 heads: 6 blocks
-// against 3, 227 and 203 us; 8 x 1057: 4 and 2, 47.8 and 42.5; 3 x 2000: 3 and 2, 60.5 and 67.2; 32 x
-// 250: 3 and 2, 16.6 and 19.1). Not with a bias,
+// against 3, 220 and 198 us; 8 x 1057: 4 and 2, 44.7 and 39.7; 3 x 2000: 3 and 2, 55.9 and 61.1; 32 x
+// 250: 3 and 2, 15.7 and 16.9). Not with a bias,
 // whose table leaves too few registers, nor under a window, where a wave of fewer queries has fewer keys
 // that others of the block need.
 static bool forward_wide(const ExactParams& p) {
@@ -669,8 +669,8 @@ int exact_splits(const ExactParams& p) {
 
 // Eight waves to a block instead of four, bf16: where every block has a CU of its own and more than two tiles to
 // a wave (a token, 12 heads: 1024 keys 10.0 us with four waves, 8.6 with eight, 701 keys 8.7 and 7.8, 300 keys,
-// 10 tiles, 7.0 and 7.1; 2 x 1024 tokens, 4 heads, forward 10.8 and 9.1, backward 27.8 and 24.7; backward
-// 2 x 256, 8 tiles, 15.0 and 16.6). Not float32, which its matrix instructions bound: 1 x 512 tokens, forward
+// 10 tiles, 7.0 and 7.1; 2 x 1024 tokens, 4 heads, forward 10.8 and 9.1, backward 27.4 and 25.1; backward
+// 2 x 256, 8 tiles, 15.1 and 17.0). Not float32, which its matrix instructions bound: 1 x 512 tokens, forward
 // and backward, 74 and 72; 4 x 201, 8 heads on 2, with a bias, 59 and 61.
 bool exact_eight_waves(int64_t blocks, int64_t tiles) { return tiles > 8 && blocks <= device_cus(); }
 

@@ -39,6 +39,9 @@ FEW = [  # B, nq, nk, heads, kv_heads, options: the same few keys or queries in 
     (64, 2, 2, 12, 12, dict(buckets=8, max_distance=5)),
     (32, 200, 6, 12, 12, dict(buckets=8, max_distance=5)),
     (32, 200, 31, 12, 12, dict(buckets=32, window=10)),
+    (24, 200, 30, 12, 12, dict(window=16, q_pos=[-70, 5, -33, 0] * 6)),  # a global query within a block
+    (24, 200, 30, 12, 4, dict(window=16, q_pos=[-70, 5, -33, 0] * 6, buckets=8, max_distance=5)),
+    (32, 30, 200, 12, 12, dict(window=16, q_pos=[-15, 40, 0, 150] * 8)),
     (1, 4100, 20, 2, 2, dict(window=16)),  # the query tiles in parts
     (1, 4100, 31, 4, 2, dict(buckets=8, max_distance=20, window=16)),
     (2, 2100, 9, 4, 1, dict(buckets=8, max_distance=20)),
